@@ -1,8 +1,10 @@
 """kvio: GPU-assisted paged-KV transfers between pinned host memory and an
-MI355X paged KV pool (Strata, Sec. 4.2 and Sec. 4.2.1).
+MI355X paged KV pool (Strata, Sec. 4.2 and Sec. 4.2.1), and the operators
+that a model runs on that pool: appending new tokens and attention.
 
 The transfer kernels and the C ABI live in ``libkvio.so`` (built from
-``csrc/`` by ``_build.py``); ``kvio`` is its ctypes binding.
+``csrc/`` by ``_build.py``); ``kvio`` is its ctypes binding.  The operators'
+kernels are in ``csrc_attn/`` (``include/kvio_attn.h``), bound by ``attn``.
 """
 from .kvio import (  # noqa: F401
     EXPORTS, HostBuffer, KVPool, KvioError, LIB_PATH,
@@ -15,4 +17,8 @@ from .kvio import (  # noqa: F401
     kvio_stream_create, kvio_stream_destroy, kvio_schedule_round, kvio_disk_prefetch, kvio_disk_store_pages, DiskPrefetch,
     KVIO_DISK_PAGE_FIRST, KVIO_DISK_LAYER_FIRST, KVIO_EIO,
     KVIO_NOALLOC_MAX_LAYERS, kvio_load_noalloc, pool_desc,
+)
+from .attn import (  # noqa: F401
+    Batch, KVIO_BF16, KVIO_FP16, KVIO_E4M3, KVIO_APPEND_INTERLEAVED, attend_workspace,
+    kvio_append, kvio_append_args, kvio_attend, kvio_attend_args, kvio_attend_workspace, kvio_batch,
 )

@@ -1,6 +1,8 @@
 """Build libkvio.so (HIP kernels + C ABI) for gfx950 with hipcc, in-tree."""
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -11,25 +13,35 @@ SOURCES = [os.path.join(CSRC, "kvio_kernels.hip"), os.path.join(CSRC, "kvio_api.
            os.path.join(CSRC, "kvio_sched.cpp"), os.path.join(CSRC, "kvio_disk.cpp"),
            os.path.join(CSRC, "kvio_staged.cpp"), os.path.join(CSRC, "kvio_noalloc.hip"),
            os.path.join(CSRC, "kvio_linkpeak.hip")]
+# the operators on the paged cache (include/kvio_attn.h), whose sources stand apart
+CSRC_ATTN = os.path.join(PKG, "csrc_attn")
+SOURCES += [os.path.join(CSRC_ATTN, f) for f in ("kvio_append.hip", "kvio_attend.hip", "kvio_attend_steps.hip", "kvio_attn_api.cpp")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Wall", "-Wextra", "-Werror", "-Wno-unused-parameter",
-    # keep the compiler from forming packed fp32 ops (there are no fp32 ops
-    # here, but every HIP source of this project is built this way)
+    # keep the compiler from forming packed fp32 ops
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-I", INCLUDE, "-I", CSRC, "-pthread",
+    "-I", INCLUDE, "-I", CSRC, "-I", os.path.join(PKG, "csrc_attn"), "-pthread",
 ]
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    """Compile every source into libkvio.so; always recompiles."""
+    """Compile every source into libkvio.so, a few at a time; always recompiles."""
     tmp = LIB + ".tmp"
-    cmd = [HIPCC] + FLAGS + list(extra) + SOURCES + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as d:
+        objects = [os.path.join(d, os.path.basename(s) + ".o") for s in SOURCES]
+        each = [f for f in FLAGS if f != "-shared"] + list(extra)
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: run([HIPCC] + each + ["-x", "hip", "-c", so[0], "-o", so[1]]), zip(SOURCES, objects)))
+        run([HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", "-pthread"] + objects + ["-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

@@ -165,6 +165,7 @@ kvio_status check_desc(const kvio_pool_desc *d, const char *fn, PoolGeom *g) {
     g->num_heads = d->num_kv_heads;
     g->host_layout = d->host_layout;
     g->seg_bytes = int64_t(d->head_dim) * d->elem_bytes;
+    g->elem_bytes = d->elem_bytes;
     g->page_size = d->page_size;
     g->num_slots = d->num_slots;
     g->row_bytes = R;

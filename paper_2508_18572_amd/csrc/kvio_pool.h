@@ -32,6 +32,7 @@ struct PoolGeom {
     int64_t num_slots;
     int64_t row_bytes;
     int64_t seg_bytes;               // head_dim * elem_bytes
+    int32_t elem_bytes;
 };
 
 // A validated span: the device-visible addresses of its chunk and page table.

@@ -1,0 +1,254 @@
+// kvio_append.hip -- new tokens' keys and values into the pages of their
+// sequences, keys and queries rotated by their positions on the way; the cache
+// in 16 bits (append_rows) or in e4m3 with a scale for each page and head
+// (append_pages, with append_rows for the queries).
+//
+// A head of D elements is D / 16 units of two pieces of 8 elements (16 bytes):
+// the two sides of 8 pairs that are rotated together, or two neighbours.  Every
+// element is read once and written once; nothing is computed that would bound this.
+#include "kvio_attn_internal.h"
+
+namespace kvio {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostPairs = 512;              // rotated pairs of a head; check in kvio_append
+constexpr double kPerTurn = 0.15915494309189533577;   // 1 / (2 pi)
+
+template <bool BF16> __device__ __forceinline__ float lo(uint32_t w) { return BF16 ? bf16_lo(w) : f16_lo(w); }
+template <bool BF16> __device__ __forceinline__ float hi(uint32_t w) { return BF16 ? bf16_hi(w) : f16_hi(w); }
+template <bool BF16> __device__ __forceinline__ uint32_t pack(float a, float b) { return BF16 ? pack_bf16(a, b) : pack_f16(a, b); }
+
+// Sine and cosine of position * inv_freq.  The product is exact in 64 bits, and
+// so many turns are taken off there: far positions lose nothing.
+__device__ __forceinline__ f32x2 sin_cos(int position, float inv_freq) {
+    const double turns = static_cast<double>(position) * static_cast<double>(inv_freq) * kPerTurn;
+    return sin_cos_of(static_cast<float>(turns - rint(turns)));
+}
+
+struct Unit {
+    u32x4 a, b;                              // 8 elements each
+};
+
+// Where unit j's pieces lie in a head and which of its pairs they hold.
+struct Place {
+    int a, b;                                // first element of each piece
+    bool turned;
+};
+__device__ __forceinline__ Place place_of(int j, int half, bool interleaved) {
+    if (interleaved || j >= half / 8) return {16 * j, 16 * j + 8, interleaved && j < half / 8};
+    return {8 * j, half + 8 * j, true};
+}
+
+template <bool BF16>
+__device__ __forceinline__ void turn(Unit &u, bool interleaved, const f32x2 *sc) {   // sc: of pairs 8 j .. 8 j + 7
+    if (!interleaved) {
+        for (int w = 0; w < 4; ++w) {
+            const f32x2 s = sc[2 * w], t = sc[2 * w + 1];
+            const float a0 = lo<BF16>(u.a[w]), a1 = hi<BF16>(u.a[w]), b0 = lo<BF16>(u.b[w]), b1 = hi<BF16>(u.b[w]);
+            u.a[w] = pack<BF16>(a0 * s.y - b0 * s.x, a1 * t.y - b1 * t.x);
+            u.b[w] = pack<BF16>(b0 * s.y + a0 * s.x, b1 * t.y + a1 * t.x);
+        }
+        return;
+    }
+    for (int w = 0; w < 8; ++w) {
+        const uint32_t word = w < 4 ? u.a[w & 3] : u.b[w & 3];
+        const float a = lo<BF16>(word), b = hi<BF16>(word);
+        const uint32_t turned = pack<BF16>(a * sc[w].y - b * sc[w].x, b * sc[w].y + a * sc[w].x);
+        if (w < 4) u.a[w & 3] = turned;
+        else u.b[w & 3] = turned;
+    }
+}
+
+__device__ __forceinline__ Unit load_unit(const uint8_t *head, const Place &p) {
+    return {*reinterpret_cast<const u32x4 *>(head + 2 * p.a), *reinterpret_cast<const u32x4 *>(head + 2 * p.b)};
+}
+__device__ __forceinline__ void store_unit(uint8_t *head, const Place &p, const Unit &u) {
+    *reinterpret_cast<u32x4 *>(head + 2 * p.a) = u.a;
+    *reinterpret_cast<u32x4 *>(head + 2 * p.b) = u.b;
+}
+
+// One workgroup a row: its angles once for all heads, then the units of its heads:
+// queries, and with CACHE keys and values too.
+template <bool BF16, bool CACHE>
+__global__ void __launch_bounds__(kThreads) append_rows(const AppendArgs a) {
+    __shared__ f32x2 sc[kMostPairs];
+    const CacheArgs &c = a.c;
+    const int row = static_cast<int>(blockIdx.x), lane = static_cast<int>(threadIdx.x) & 63;
+    const int b = seq_with_row(c, row, lane);
+    if (b < 0) return;
+    const Seq s = seq_of(c, b);
+    const int at = s.first + row - s.row0;
+    if (row < s.row0 || row >= s.row0 + s.rows || at < 0) return;
+    const int position = a.positions != nullptr ? a.positions[row] : at;
+    for (int i = static_cast<int>(threadIdx.x); i < a.rot_half; i += kThreads) sc[i] = sin_cos(position, a.inv_freq[i]);
+    workgroup_barrier();
+
+    int64_t slot = -1;
+    if (CACHE) {
+        const int page = page_of(c, b, at);
+        if (page >= 0) slot = int64_t(page) * c.page_size + (at - static_cast<int>(div_by(static_cast<uint32_t>(at), c.page_div)) * c.page_size);
+    }
+    const int units = c.head_dim / 16, heads = a.q_heads + (CACHE ? 2 * c.heads : 0);
+    const int64_t seg = int64_t(c.head_dim) * 2, cache_row = seg * c.heads;
+    for (int i = static_cast<int>(threadIdx.x); i < heads * units; i += kThreads) {
+        const int h = i / units, j = i - h * units, kh = h - a.q_heads, vh = kh - c.heads;
+        const bool is_v = vh >= 0;
+        const Place p = place_of(j, is_v ? 0 : a.rot_half, a.interleaved);
+        const uint8_t *from;
+        uint8_t *to;
+        if (kh < 0) {
+            from = a.q + row * a.q_stride + h * seg;
+            to = a.q_out + row * a.q_out_stride + h * seg;
+        } else {
+            if (slot < 0) continue;
+            from = is_v ? a.v + row * a.v_stride + vh * seg : a.k + row * a.k_stride + kh * seg;
+            to = is_v ? c.v_cache + slot * cache_row + vh * seg : c.k_cache + slot * cache_row + kh * seg;
+        }
+        Unit u = load_unit(from, p);
+        if (p.turned) turn<BF16>(u, a.interleaved, sc + 8 * j);
+        store_unit(to, p, u);
+    }
+}
+
+// The smallest power of two, 2^-100 at least, with `top` within 448 of it.
+__device__ __forceinline__ float scale_for(float top) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, top);
+    // 448 = 1.75 * 2^8: one more where the mantissa passes 0.75
+    const int e = static_cast<int>(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+    return __builtin_bit_cast(float, static_cast<uint32_t>((e < -100 ? -100 : e) + 127) << 23);
+}
+
+// v * inv as an e4m3 value: within +-448, NaN kept.
+__device__ __forceinline__ float within(float v) { return v != v ? v : fminf(fmaxf(v, -448.0f), 448.0f); }
+
+__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) <= 3.4e38f ? fabsf(v) : 0.0f; }
+
+template <bool BF16>
+__device__ __forceinline__ u32x2 codes_of(u32x4 x, float inv) {
+    u32x2 r;
+    for (int w = 0; w < 2; ++w)
+        r[w] = pack_e4m3(within(lo<BF16>(x[2 * w]) * inv), within(hi<BF16>(x[2 * w]) * inv),
+                         within(lo<BF16>(x[2 * w + 1]) * inv), within(hi<BF16>(x[2 * w + 1]) * inv));
+    return r;
+}
+
+// One wave for K or V of one head in one page that new tokens reach: their
+// largest element, the page's scale, its older rows again where that grew, the new rows.
+template <bool BF16>
+__global__ void __launch_bounds__(kThreads) append_pages(const AppendArgs a) {
+    const CacheArgs &c = a.c;
+    const int lane = static_cast<int>(threadIdx.x) & 63;
+    const int64_t wave = int64_t(blockIdx.x) * (kThreads / 64) + wave_first(static_cast<int>(threadIdx.x) >> 6);
+    int item = static_cast<int>(wave / (2 * c.heads));
+    const int part = static_cast<int>(wave - int64_t(item) * 2 * c.heads), h = part >> 1;
+    const bool is_v = (part & 1) != 0;
+    if (item >= a.page_items) return;
+    // The item-th page of all that sequences reach, in order.
+    int b = -1, page_at = 0;
+    for (int i = 0; i < c.num_seqs && b < 0; i += 64) {
+        int pages = 0, first = 0;
+        if (i + lane < c.num_seqs) {
+            const Seq s = seq_of(c, i + lane);
+            const int from = s.first > 0 ? s.first : 0, to = s.first + s.rows;    // tokens [from, to)
+            if (to > from) {
+                first = static_cast<int>(div_by(static_cast<uint32_t>(from), c.page_div));
+                pages = static_cast<int>(div_by(static_cast<uint32_t>(to - 1), c.page_div)) - first + 1;
+            }
+        }
+        const int upto = lanes_upto(pages, lane);
+        const uint64_t behind = wave_ballot(upto > item);
+        if (behind != 0) {
+            const int at = __builtin_ctzll(behind);
+            b = i + at;
+            page_at = wave_read(first, at) + item - (wave_read(upto, at) - wave_read(pages, at));
+        }
+        item -= wave_read(upto, 63);
+    }
+    if (b < 0) return;
+    const Seq s = seq_of(c, b);
+    const int P = c.page_size, begin = page_at * P;
+    const int from = s.first > begin ? s.first : begin, to = s.first + s.rows < begin + P ? s.first + s.rows : begin + P;
+    const int page = page_of(c, b, begin);
+    if (page < 0) return;
+
+    const int units = c.head_dim / 16;
+    int span = 1;                            // lanes of a row
+    while (span < units) span *= 2;
+    const int per_pass = 64 / span, j = lane & (span - 1), sub = lane / span;
+    const int64_t seg = c.head_dim, cache_row = seg * c.heads;
+    uint8_t *cache = (is_v ? c.v_cache : c.k_cache) + (int64_t(page) * P) * cache_row + h * seg;
+    const uint8_t *in = is_v ? a.v : a.k;
+    const int64_t in_stride = is_v ? a.v_stride : a.k_stride;
+    const Place p = place_of(j < units ? j : 0, is_v ? 0 : a.rot_half, a.interleaved);
+    auto fetch = [&](int t) {                // the lane's unit of context token t, rotated, in the model's type
+        const int row = s.row0 + (t - s.first);
+        Unit u = load_unit(in + row * in_stride + h * seg * 2, p);
+        if (p.turned) {
+            const int position = a.positions != nullptr ? a.positions[row] : t;
+            f32x2 sc[8];
+            for (int e = 0; e < 8; ++e) sc[e] = sin_cos(position, a.inv_freq[8 * j + e]);
+            turn<BF16>(u, a.interleaved, sc);
+        }
+        return u;
+    };
+    float *at = (is_v ? c.v_scale : c.k_scale) + page * c.scale_stride + h;
+    const float was = from != begin ? *at : 0.0f;   // read by all lanes before one of them writes it
+    float top = 0;
+    for (int t = from + sub; t < to; t += per_pass) {
+        if (j >= units) continue;
+        const Unit u = fetch(t);
+        for (int w = 0; w < 4; ++w) {
+            top = fmaxf(top, fmaxf(finite_abs(lo<BF16>(u.a[w])), finite_abs(hi<BF16>(u.a[w]))));
+            top = fmaxf(top, fmaxf(finite_abs(lo<BF16>(u.b[w])), finite_abs(hi<BF16>(u.b[w]))));
+        }
+    }
+    for (int by = 1; by < 64; by *= 2) top = fmaxf(top, lane_xor(top, by));
+    float scale = scale_for(top);
+    if (from != begin) {
+        if (top <= 448.0f * was) {
+            scale = was;
+        } else {
+            const float by = was / scale;    // below one
+            for (int t = sub; t < from - begin; t += per_pass) {
+                if (j >= units) continue;
+                u32x4 *row = reinterpret_cast<u32x4 *>(cache + t * cache_row + 16 * j);
+                u32x4 x = *row;
+                for (int w = 0; w < 4; ++w) {
+                    const f32x2 l = e4m3_f32<false>(x[w]), m = e4m3_f32<true>(x[w]);
+                    x[w] = pack_e4m3(within(l.x * by), within(l.y * by), within(m.x * by), within(m.y * by));
+                }
+                *row = x;
+            }
+        }
+    }
+    if (lane == 0 && scale != was) *at = scale;
+    const float inv = 1.0f / scale;
+    for (int t = from + sub; t < to; t += per_pass) {
+        if (j >= units) continue;
+        const Unit u = fetch(t);
+        uint8_t *row = cache + (t - begin) * cache_row;
+        *reinterpret_cast<u32x2 *>(row + p.a) = codes_of<BF16>(u.a, inv);
+        *reinterpret_cast<u32x2 *>(row + p.b) = codes_of<BF16>(u.b, inv);
+    }
+}
+
+template <bool BF16>
+hipError_t launch(const AppendArgs &a, bool e4m3, hipStream_t stream) {
+    if (!e4m3)
+        hipLaunchKernelGGL((append_rows<BF16, true>), dim3(a.c.num_tokens), dim3(kThreads), 0, stream, a);
+    else {
+        const int64_t waves = int64_t(a.page_items) * 2 * a.c.heads;
+        hipLaunchKernelGGL((append_pages<BF16>), dim3(static_cast<unsigned>((waves + 3) / 4)), dim3(kThreads), 0, stream, a);
+        if (a.q_heads > 0) hipLaunchKernelGGL((append_rows<BF16, false>), dim3(a.c.num_tokens), dim3(kThreads), 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendArgs &a, int32_t dtype, bool e4m3, hipStream_t stream) {
+    return dtype == KVIO_BF16 ? launch<true>(a, e4m3, stream) : launch<false>(a, e4m3, stream);
+}
+
+}  // namespace kvio

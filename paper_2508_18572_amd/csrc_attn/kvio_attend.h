@@ -1,0 +1,113 @@
+// kvio_attend.h -- what the attention kernels share on the device.
+#pragma once
+
+#include "kvio_attn_internal.h"
+
+namespace kvio {
+
+constexpr float kMinusInf = -__builtin_huge_valf();
+constexpr int kTile = 32;                    // keys that a wave takes at a time
+// A running maximum stays until a score passes it by this much (in powers of two): probabilities
+// and their sums stay below 2^8 times the number of keys, and rescaling is rare.
+constexpr float kSlack = 8.0f;
+
+// The keys of a sequence: those that any row sees, [lo, hi), and those that all see.
+struct Span {
+    int32_t lo, hi, whole_lo, whole_hi;
+    int32_t tiles;                           // of kTile keys, at multiples of it, that hold [lo, hi)
+};
+__device__ __forceinline__ Span span_of(const AttendArgs &a, const Seq &s) {
+    Span r;
+    const int last = s.first + s.rows - 1;   // the last row's place
+    r.hi = last + 1;
+    r.lo = a.window > 0 && s.first - a.window + 1 > 0 ? s.first - a.window + 1 : 0;
+    r.whole_lo = a.window > 0 && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
+    r.whole_hi = s.first + 1;
+    r.tiles = s.rows > 0 && r.hi > r.lo ? (r.hi + kTile - 1) / kTile - r.lo / kTile : 0;
+    return r;
+}
+
+// All sequences' tiles, end to end, cut into equal ranges.
+struct Ranges {
+    int32_t total, per_worker;
+};
+// `begin` (if not null): the first tile of sequence b.
+__device__ __forceinline__ Ranges ranges_of(const AttendArgs &a, int lane, int b = 0, int64_t *begin = nullptr) {
+    int all = 0, before = 0;
+    for (int i = lane; i < a.c.num_seqs; i += 64) {
+        const int t = span_of(a, seq_of(a.c, i)).tiles;
+        all += t;
+        before += i < b ? t : 0;
+    }
+    for (int by = 1; by < 64; by *= 2) {
+        all += lane_xor(all, by);
+        if (begin != nullptr) before += lane_xor(before, by);
+    }
+    if (begin != nullptr) *begin = wave_first(before);
+    Ranges r;
+    r.total = wave_first(all);
+    r.per_worker = (r.total + a.workers - 1) / a.workers;
+    if (r.per_worker < a.min_tiles) r.per_worker = a.min_tiles;
+    return r;
+}
+// The sequence that holds tile `at` (one does), and where its tiles begin.
+__device__ __forceinline__ int find_tile(const AttendArgs &a, int64_t at, int lane, int64_t *begin) {
+    int64_t before = 0;
+    for (int i = 0;; i += 64) {
+        const int t = i + lane < a.c.num_seqs ? span_of(a, seq_of(a.c, i + lane)).tiles : 0;
+        const int upto = lanes_upto(t, lane);
+        const uint64_t behind = wave_ballot(before + upto > at);
+        if (behind != 0) {
+            const int l = __builtin_ctzll(behind);
+            *begin = before + wave_read(upto, l) - wave_read(t, l);
+            return i + l;
+        }
+        before += wave_read(upto, 63);
+    }
+}
+
+// Floats into the partial results: of a worker, head and one of its two shared sequences, a row's
+// sums, then its maximum and the sum of its probabilities.
+__device__ __forceinline__ int64_t partial_at(const AttendArgs &a, int worker, int h, int which, int row, int dim) {
+    return (((int64_t(worker) * a.c.heads + h) * 2 + which) * a.slot_rows + row) * (dim + 2);
+}
+
+__device__ __forceinline__ float lse_of(float top, float sum) {
+    return sum == 0 ? kMinusInf : (top + log2_fast(sum)) * 0.69314718055994530942f;
+}
+
+// Rows of sequences of which no row sees a key: zeros, by one wave for a KV head.
+__device__ __forceinline__ void rows_without_keys(const AttendArgs &a, int h, int lane) {
+    for (int b = 0; b < a.c.num_seqs; ++b) {
+        const Seq s = seq_of(a.c, b);
+        if (s.rows <= 0 || span_of(a, s).tiles != 0) continue;
+        for (int i = 0; i < s.rows * a.group; ++i) {
+            const int token = i / a.group, qh = h * a.group + i - token * a.group;
+            for (int d = lane; d < a.c.head_dim; d += 64)
+                reinterpret_cast<uint16_t *>(a.out + (s.row0 + token) * a.out_stride)[int64_t(qh) * a.c.head_dim + d] = 0;
+            if (a.lse != nullptr && lane == 0) a.lse[int64_t(s.row0 + token) * a.q_heads + qh] = kMinusInf;
+        }
+    }
+}
+
+// Ones where an element of the word, two of 16 bits or four codes, is infinite or NaN.
+template <bool BF16, bool E4M3>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    if constexpr (E4M3) {
+        const uint32_t m = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // codes 0x7f and 0xff
+        return (m >> 7) * 0xffu;
+    } else {
+        constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+        return ((w & kExp) == kExp ? 0xffffu : 0u) | (((w >> 16) & kExp) == kExp ? 0xffff0000u : 0u);
+    }
+}
+
+// Element i of a row of the cache.
+template <bool BF16, bool E4M3>
+__device__ __forceinline__ float element(const uint8_t *p, int i) {
+    if constexpr (E4M3) return e4m3_f32<false>(p[i]).x;
+    const uint32_t u = reinterpret_cast<const uint16_t *>(p)[i];
+    return BF16 ? bf16_lo(u) : f16_lo(u);
+}
+
+}  // namespace kvio

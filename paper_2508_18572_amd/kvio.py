@@ -438,7 +438,11 @@ class HostBuffer:
 
 class KVPool:
     """A pool handle over a torch tensor shaped (2, L, S, H, D): K then V, each
-    layer a token-major (S, H, D) array of 16-bit elements.
+    layer a token-major (S, H, D) array of 16-bit or 8-bit elements.
+
+    append and attend take pools of bfloat16, float16 and, with scales, float8_e4m3fn (or
+    uint8 codes): scales is float32 (2, L, S / page_size, H), one for each page
+    and head, whose rows of heads may lie apart.
 
     load_launch / offload_launch shape each direction (see launch(); a
     KVIO_LAUNCH_STAGED flag stages that direction through HBM slots of
@@ -447,10 +451,14 @@ class KVPool:
 
     def __init__(self, pool: "torch.Tensor", page_size: int,
                  load_launch: Optional[kvio_launch] = None, offload_launch: Optional[kvio_launch] = None,
-                 host_layout: int = KVIO_HOST_TOKEN_MAJOR, staging_bytes: int = 0):
+                 host_layout: int = KVIO_HOST_TOKEN_MAJOR, staging_bytes: int = 0,
+                 scales: Optional["torch.Tensor"] = None):
         assert pool.is_cuda and pool.is_contiguous() and pool.dim() == 5 and pool.shape[0] == 2
         _, L, S, H, D = pool.shape
-        self.tensor = pool
+        if scales is not None:
+            assert pool.dtype in (torch.float8_e4m3fn, torch.uint8) and scales.dtype == torch.float32
+            assert scales.device == pool.device and scales.shape == (2, L, S // page_size, H) and scales.stride(3) == 1
+        self.tensor, self.scales = pool, scales
         self.num_layers, self.num_slots, self.page_size = L, S, page_size
         self.row_bytes = H * D * pool.element_size()
         self.handle = kvio_pool_create(L, H, D, pool.element_size(), page_size, S,
@@ -467,6 +475,23 @@ class KVPool:
 
     def load_layer(self, spans, layer, stream=None, done=None):
         kvio_load_layer(self.handle, spans, layer, stream, done)
+
+    def append(self, layer, batch, k, v, q=None, q_out=None, inv_freq=None, positions=None, interleaved=False,
+               stream=None):
+        """Write new tokens' k and v, (N, H, D), into the pages of their sequences (an attn.Batch), rotating k
+        and q, (N, heads, D), on the way by position * inv_freq (float32, half as many as elements are rotated; None:
+        no rotation).  Positions are the tokens' places, or positions, int32 (N,).  Tokens may lie apart
+        (slices of a fused projection).  Returns q_out: rotated q, new unless given; q itself is allowed."""
+        from . import attn
+        return attn.append(self, layer, batch, k, v, q, q_out, inv_freq, positions, interleaved, stream)
+
+    def attend(self, layer, batch, q, out=None, lse=None, scale=None, window=0, workspace=None, stream=None):
+        """Causal attention of the new tokens' q, (N, heads, D), over their contexts in `layer`, their own
+        keys and values (appended before) included.  scale: of the scores, 1 / sqrt(D) unless given; window: the
+        last so many tokens only.  lse: float32 (N, heads) for the logarithms of the softmax's sums.  workspace:
+        memory of attn.attend_workspace bytes, for calls one after the other; new unless given."""
+        from . import attn
+        return attn.attend(self, layer, batch, q, out, lse, scale, window, workspace, stream)
 
     def check(self):
         kvio_check(self.handle)
