@@ -15,7 +15,7 @@ SOURCES = [os.path.join(CSRC, "kvio_kernels.hip"), os.path.join(CSRC, "kvio_api.
            os.path.join(CSRC, "kvio_linkpeak.hip")]
 # the operators on the paged cache (include/kvio_attn.h), whose sources stand apart
 CSRC_ATTN = os.path.join(PKG, "csrc_attn")
-SOURCES += [os.path.join(CSRC_ATTN, f) for f in ("kvio_append.hip", "kvio_attend.hip", "kvio_attend_steps.hip", "kvio_attn_api.cpp")]
+SOURCES += [os.path.join(CSRC_ATTN, f) for f in ("kvio_append.hip", "kvio_attend_steps.hip", "kvio_attend_blocks.hip", "kvio_attn_api.cpp")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -23,6 +23,8 @@ FLAGS = [
     "-Wall", "-Wextra", "-Werror", "-Wno-unused-parameter",
     # keep the compiler from forming packed fp32 ops
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    # matrix products in either kind of registers: attention reads their results with ordinary instructions
+    "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-I", INCLUDE, "-I", CSRC, "-I", os.path.join(PKG, "csrc_attn"), "-pthread",
 ]
 

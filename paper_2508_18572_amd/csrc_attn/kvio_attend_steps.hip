@@ -400,11 +400,10 @@ hipError_t launch_steps(const AttendArgs &a, const AttendPlan &plan, int32_t dty
     return e4m3 ? launch_dim<false, true>(a, plan, stream) : launch_dim<false, false>(a, plan, stream);
 }
 
-AttendPlan plan_attend(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx) {
+AttendPlan plan_steps(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx) {
     AttendPlan p = {};
     const int64_t rows = int64_t(max_query) * (q_heads / heads);
-    p.few = rows <= (dim <= 128 ? 64 : 32);
-    if (!p.few) return p;
+    p.few = true;
     p.columns = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     p.heads_per_group = heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
     const int64_t head_groups = heads / p.heads_per_group, splits = kWaves / p.heads_per_group;

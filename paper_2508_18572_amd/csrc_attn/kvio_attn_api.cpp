@@ -129,6 +129,9 @@ kvio_status check_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *a
     if (dim != 64 && dim != 128 && dim != 256) return fail(KVIO_EINVAL, "%s: heads of %lld dims; 64, 128 and 256 are built", fn, (long long)dim);
     if (args->num_q_heads < p->g.num_heads || args->num_q_heads % p->g.num_heads != 0 || args->num_q_heads > 65536)
         return fail(KVIO_EINVAL, "%s: %d query heads are no multiple of the pool's %d", fn, args->num_q_heads, p->g.num_heads);
+    const int32_t group = args->num_q_heads / p->g.num_heads;
+    if (group > kvio::block_rows(static_cast<int>(dim)))
+        return fail(KVIO_EINVAL, "%s: %d query heads to a KV head; up to %d are built", fn, group, kvio::block_rows(static_cast<int>(dim)));
     if (args->window < 0) return fail(KVIO_EINVAL, "%s: window %d < 0", fn, args->window);
     if (!(args->softmax_scale > 0) || !isfinite(args->softmax_scale)) return fail(KVIO_EINVAL, "%s: softmax_scale must be positive and finite", fn);
     if (args->reserved != 0) return fail(KVIO_EINVAL, "%s: reserved is not 0", fn);
@@ -140,10 +143,15 @@ kvio_status check_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *a
     return KVIO_OK;
 }
 
+// Rows of a KV head that kvio_attend_steps.hip holds in a wave's registers, by the size of heads.
+int64_t most_step_rows(int64_t dim) { return dim <= 128 ? 64 : 32; }
+
 kvio::AttendPlan plan_of(kvio_pool_t p, const kvio_attend_args &args) {
     const kvio::PoolGeom &g = p->g;
-    return kvio::plan_attend(args.cache_dtype == KVIO_E4M3, g.num_heads, args.num_q_heads, static_cast<int32_t>(g.seg_bytes / g.elem_bytes), args.batch,
-                             longest_query(args.batch), args.batch.max_pages * g.page_size);
+    const int32_t dim = static_cast<int32_t>(g.seg_bytes / g.elem_bytes), longest = longest_query(args.batch), max_ctx = args.batch.max_pages * g.page_size;
+    if (int64_t(longest) * (args.num_q_heads / g.num_heads) <= most_step_rows(dim))
+        return kvio::plan_steps(args.cache_dtype == KVIO_E4M3, g.num_heads, args.num_q_heads, dim, args.batch, longest, max_ctx);
+    return kvio::plan_blocks(g.num_heads, args.num_q_heads, dim, args.batch, longest, max_ctx);
 }
 
 }  // namespace
@@ -244,11 +252,13 @@ kvio_status kvio_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *ar
     a.workers = plan.workers;
     a.min_tiles = plan.min_tiles;
     a.slot_rows = plan.slot_rows;
+    a.block_tokens = plan.block_tokens;
+    a.min_keys = plan.min_keys;
     if (args->workspace_bytes < plan.bytes)
         return fail(KVIO_EINVAL, "%s: workspace of %llu bytes, %llu are needed", fn, (unsigned long long)args->workspace_bytes, (unsigned long long)plan.bytes);
     st = check_array(p, args->workspace, plan.bytes, 16, fn, "workspace");
     if (st != KVIO_OK) return st;
-    const hipError_t e = kvio::launch_attend(a, plan, args->dtype, e4m3, stream);
+    const hipError_t e = (plan.few ? kvio::launch_steps : kvio::launch_blocks)(a, plan, args->dtype, e4m3, stream);
     return e == hipSuccess ? KVIO_OK : kvio::fail_hip(e, fn);
 }
 

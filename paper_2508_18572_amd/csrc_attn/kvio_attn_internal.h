@@ -51,22 +51,27 @@ struct AttendArgs {
     // How the work is split (AttendPlan).
     float *partials;
     int32_t heads_per_group, workers, min_tiles, slot_rows;
+    int32_t block_tokens, min_keys;
 };
 
 // How a call of given sizes is split; what it needs of workspace.
 struct AttendPlan {
-    bool few;                      // few rows to a sequence: kvio_attend_steps.hip
+    bool few;                      // few rows to a sequence: kvio_attend_steps.hip, else kvio_attend_blocks.hip
     int32_t columns;               // blocks of 16 rows that a wave holds
     int32_t heads_per_group, workers, min_tiles, slot_rows;
+    int32_t block_tokens, min_keys;
     uint32_t groups;               // workgroups
     bool joined;                   // partial results may be left
     uint64_t bytes;
 };
-AttendPlan plan_attend(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
+// Rows that a workgroup of kvio_attend_blocks.hip holds: out^T of a wave's share takes half the registers.
+constexpr int block_rows(int dim) { return dim <= 128 ? 256 : 128; }
+AttendPlan plan_steps(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
+AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
 
 hipError_t launch_append(const AppendArgs &a, int32_t dtype, bool e4m3, hipStream_t stream);
-hipError_t launch_attend(const AttendArgs &a, const AttendPlan &plan, int32_t dtype, bool e4m3, hipStream_t stream);
 hipError_t launch_steps(const AttendArgs &a, const AttendPlan &plan, int32_t dtype, bool e4m3, hipStream_t stream);
+hipError_t launch_blocks(const AttendArgs &a, const AttendPlan &plan, int32_t dtype, bool e4m3, hipStream_t stream);
 
 // ---- shared by the kernels -----------------------------------------------------------
 
@@ -106,10 +111,24 @@ __device__ __forceinline__ int seq_with_row(const CacheArgs &c, int row, int lan
     return b < c.num_seqs ? b : -1;
 }
 
+// 64-bit values between lanes, by halves.
+__device__ __forceinline__ int64_t whole_of(int lo, int hi) { return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo)); }
+__device__ __forceinline__ int64_t lane_xor(int64_t v, int mask) { return whole_of(lane_xor(static_cast<int>(v), mask), lane_xor(static_cast<int>(v >> 32), mask)); }
+__device__ __forceinline__ int64_t wave_read(int64_t v, int lane) { return whole_of(wave_read(static_cast<int>(v), lane), wave_read(static_cast<int>(v >> 32), lane)); }
+__device__ __forceinline__ int64_t wave_first(int64_t v) { return whole_of(wave_first(static_cast<int>(v)), wave_first(static_cast<int>(v >> 32))); }
+
 // Sum of this and all lower lanes' values.
 __device__ __forceinline__ int lanes_upto(int v, int lane) {
     for (int by = 1; by < 64; by *= 2) {
         const int other = lane_up(v, by);
+        if (lane >= by) v += other;
+    }
+    return v;
+}
+
+__device__ __forceinline__ int64_t lanes_upto(int64_t v, int lane) {
+    for (int by = 1; by < 64; by *= 2) {
+        const int64_t other = whole_of(lane_up(static_cast<int>(v), by), lane_up(static_cast<int>(v >> 32), by));
         if (lane >= by) v += other;
     }
     return v;

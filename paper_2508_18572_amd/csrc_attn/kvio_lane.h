@@ -67,6 +67,14 @@ __device__ __forceinline__ f32x16 product32(u32x4 a, u32x4 b, f32x16 c) {
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// Four 16-bit elements a lane from LDS, turned: each group of 16 lanes names 4 rows of 16 elements, lane i the elements
+// 4 (i % 4) .. + 3 of row i / 4, and lane i gets element i of the rows, in their order.
+__device__ __forceinline__ u32x2 lds_turned(const uint8_t *p) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p)));
+}
+
 // ---- between lanes -------------------------------------------------------------------
 __device__ __forceinline__ float lane_xor(float v, int mask) { return __shfl_xor(v, mask); }
 __device__ __forceinline__ int lane_read(int v, int lane) { return __shfl(v, lane); }       // `lane` may differ by lane

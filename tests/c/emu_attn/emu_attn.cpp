@@ -12,7 +12,7 @@
 
 namespace {
 
-constexpr size_t kStack = 128 << 10;
+constexpr size_t kStack = 1 << 20;
 constexpr const char *kBarrier = "barrier";
 
 struct Thread {

@@ -87,33 +87,55 @@ float emu_16(const uint32_t *words, int i) {
     const uint32_t w = words[i / 2];
     return i & 1 ? (BF16 ? bf16_hi(w) : f16_hi(w)) : (BF16 ? bf16_lo(w) : f16_lo(w));
 }
+// The lane's 8 elements of each operand go to the others as floats.
+template <bool BF16>
+const char *emu_operands(u32x4 a, u32x4 b, const char *what) {
+    uint32_t words[8];
+    float both[16];
+    memcpy(words, &a, 16);
+    memcpy(words + 4, &b, 16);
+    for (int i = 0; i < 16; ++i) both[i] = emu_16<BF16>(words, i);
+    return emu_attn_join(both, sizeof both, what);
+}
+inline const float *emu_of(const char *all, int lane) { return reinterpret_cast<const float *>(all + lane * 64); }
 template <bool BF16>
 f32x4 product16(u32x4 a, u32x4 b, f32x4 c) {
-    uint32_t both[8];
-    memcpy(both, &a, 16);
-    memcpy(both + 4, &b, 16);
-    const char *all = emu_attn_join(both, sizeof both, "product16");
+    const char *all = emu_operands<BF16>(a, b, "product16");
     const int l = emu_attn_lane();
-    for (int r = 0; r < 4; ++r)
-        for (int g = 0; g < 4; ++g)
-            for (int i = 0; i < 8; ++i)
-                c[r] += emu_16<BF16>(reinterpret_cast<const uint32_t *>(all + (16 * g + 4 * (l / 16) + r) * 64), i) *
-                        emu_16<BF16>(reinterpret_cast<const uint32_t *>(all + (16 * g + l % 16) * 64) + 4, i);
+    for (int g = 0; g < 4; ++g) {
+        const float *y = emu_of(all, 16 * g + l % 16) + 8;
+        for (int r = 0; r < 4; ++r) {
+            const float *x = emu_of(all, 16 * g + 4 * (l / 16) + r);
+            for (int i = 0; i < 8; ++i) c[r] += x[i] * y[i];
+        }
+    }
     return c;
 }
 template <bool BF16>
 f32x16 product32(u32x4 a, u32x4 b, f32x16 c) {
-    uint32_t both[8];
-    memcpy(both, &a, 16);
-    memcpy(both + 4, &b, 16);
-    const char *all = emu_attn_join(both, sizeof both, "product32");
+    const char *all = emu_operands<BF16>(a, b, "product32");
     const int l = emu_attn_lane();
-    for (int r = 0; r < 16; ++r)
-        for (int g = 0; g < 2; ++g)
-            for (int i = 0; i < 8; ++i)
-                c[r] += emu_16<BF16>(reinterpret_cast<const uint32_t *>(all + (32 * g + 8 * (r / 4) + 4 * (l / 32) + r % 4) * 64), i) *
-                        emu_16<BF16>(reinterpret_cast<const uint32_t *>(all + (32 * g + l % 32) * 64) + 4, i);
+    for (int g = 0; g < 2; ++g) {
+        const float *y = emu_of(all, 32 * g + l % 32) + 8;
+        for (int r = 0; r < 16; ++r) {
+            const float *x = emu_of(all, 32 * g + 8 * (r / 4) + 4 * (l / 32) + r % 4);
+            float sum = 0;
+            for (int i = 0; i < 8; ++i) sum += x[i] * y[i];
+            c[r] += sum;
+        }
+    }
     return c;
+}
+// Each group of 16 lanes: lane 4 r + i names elements 4 i .. 4 i + 3 of row r, and gets element 4 r + i of all four.
+inline u32x2 lds_turned(const uint8_t *p) {
+    uint16_t mine[4], got[4];
+    memcpy(mine, p, 8);
+    const char *all = emu_attn_join(mine, sizeof mine, "lds_turned");
+    const int l = emu_attn_lane(), i = l % 16;
+    for (int r = 0; r < 4; ++r) memcpy(&got[r], all + (l - i + 4 * r + i / 4) * 64 + 2 * (i % 4), 2);
+    u32x2 v;
+    memcpy(&v, got, 8);
+    return v;
 }
 
 template <class T>
