@@ -29,7 +29,7 @@
 namespace kvio {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 constexpr int kJoinRows = 16;                            // rows that a workgroup joins
 
 // The blocks of one sequence and the keys that each goes through.
@@ -116,20 +116,28 @@ __device__ __forceinline__ Where where_is(const AttendArgs &a, const Line &l, in
 // Floats into the partial results of a workgroup: of each row its sums, behind all rows' the maximum and the sum of
 // probabilities.  `which`: the block began before its range (0), or goes on after it (1).
 __device__ __forceinline__ int64_t block_partial_at(const AttendArgs &a, int worker, int which, int dim) {
-    return (int64_t(worker) * 2 + which) * a.slot_rows * (dim + 2);
+    return int64_t(a.workers) * 4 + (int64_t(worker) * 2 + which) * a.slot_rows * (dim + 2);
 }
+// Before them, for each workgroup: the block that its range is the first to cut, and how many others have a share of it; 0: none.
+struct alignas(16) Cut {
+    int32_t h, b, j, others;
+};
+
+constexpr int waves_of(int dim) { return dim <= 128 ? 8 : 4; }
 
 template <bool BF16, bool E4M3, int D>
 struct Shape {
     static constexpr int kElem = E4M3 ? 1 : 2, kSeg = D * kElem;
-    static constexpr int kKeys = D <= 128 ? 64 : 32, kHalves = kKeys / 32;   // keys of a tile
+    static constexpr int kKeys = 64;                     // of a tile
+    static constexpr int kWaves = waves_of(D), kThreads = 64 * kWaves;
     static constexpr int kWaveRows = block_rows(D) / kWaves, kColumns = kWaveRows / 32;   // rows to a wave, 32 to a column of products
     static constexpr int kSteps = D / 16, kDimBlocks = D / 32;
-    static constexpr int kPieces = kSeg / 16, kRowsAtOnce = kThreads / kPieces, kPasses = kKeys / kRowsAtOnce;
+    static constexpr int kPieces = kSeg / 16, kRowsAtOnce = std::min(kKeys, kThreads / kPieces), kPasses = kKeys / kRowsAtOnce;
     // 16 rows' pieces of 16 bytes lie in all banks; so do 32 bytes of 8 rows
     static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 64;
     static constexpr bool kPBf16 = BF16 || E4M3;
-    static constexpr int kKBuffers = 1 + kHalves;        // the second half's scores are computed after the next tile's K is due
+    // Operands in registers at a time; with fewer than a phase has, K of a tile is still read while the next but one is put.
+    static constexpr int kKOps = D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 4 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
     struct alignas(16) Lds {
         uint8_t k[kKBuffers][kKeys * kKRow], v[2][kKeys * kVRow];
         float k_scale[4][64], v_scale[4][64];            // of tiles, by their number & 3
@@ -138,7 +146,7 @@ struct Shape {
 };
 
 template <bool BF16, bool E4M3, int D>
-__global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a) {
+__global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_blocks(const AttendArgs a) {
     using S = Shape<BF16, E4M3, D>;
     constexpr int kKeys = S::kKeys, kColumns = S::kColumns, kWaveRows = S::kWaveRows;
     __shared__ typename S::Lds lds;
@@ -151,7 +159,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
     const Line line = line_of(a, lane);
     int64_t pos = worker * line.per_worker;
     const int64_t stop = pos + line.per_worker < line.all ? pos + line.per_worker : line.all;
-    if (pos >= stop) return;
+    Cut cut = {0, 0, 0, 0};
+    Cut *my_cut = reinterpret_cast<Cut *>(a.partials) + worker;
+    if (pos >= stop) {
+        if (a.joined && tid == 0) *my_cut = cut;
+        return;
+    }
     if (tid < 4) lds.odd[tid] = -1;
     int serial = 0;                                      // tiles so far
     Where at = where_is(a, line, pos, lane);
@@ -172,6 +185,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
         const int to_tile = stop >= next ? all_tiles : static_cast<int>(lo + (stop - at.begin)) / kKeys - tile0;
         const int block_row0 = at.j * a.block_tokens;    // in the sequence
         const int n = to_tile - from_tile;
+        if (from_tile == 0 && to_tile < all_tiles && to_tile > 0)
+            cut = Cut{h, b, at.j, static_cast<int>((next - 1 - stop) / line.per_worker) + 1};
         at.begin = pos = next;
         ++at.j;
         if (n <= 0) continue;
@@ -185,13 +200,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
         const int wave_first_place = first + static_cast<int>(div_by(static_cast<uint32_t>(wave_row0), a.group_div));
         const int wave_last_place = first + static_cast<int>(div_by(static_cast<uint32_t>(idle ? 0 : wave_row1), a.group_div));
 
+        int g16 = 16 * g;
+        keep_here(g16);
         int place[kColumns];                             // of the lane's columns; below any key for none
         u32x4 q[kColumns][S::kSteps];
 #pragma unroll
         for (int t = 0; t < kColumns; ++t) {
             const int row = wave_row0 + 32 * t + m, token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div));
             place[t] = row < rows ? first + token : -1;
-            const uint8_t *p = a.q + (s.row0 + block_row0 + token) * a.q_stride + int64_t(h * a.group + row - token * a.group) * (2 * D) + 16 * g;
+            const uint8_t *p = a.q + (s.row0 + block_row0 + token) * a.q_stride + int64_t(h * a.group + row - token * a.group) * (2 * D) + g16;
 #pragma unroll
             for (int i = 0; i < S::kSteps; ++i) q[t][i] = row < rows ? *reinterpret_cast<const u32x4 *>(p + 32 * i) : u32x4{0, 0, 0, 0};
         }
@@ -208,181 +225,163 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
         }
 
         // ---- keys and values on their way into LDS ----------------------------------------
-        const int lane_key = lane & (kKeys - 1);         // the key of a tile whose page the lane looks up
-        auto page_in = [&](int tile) KVIO_INLINE {                   // -2 for a key that no row sees
-            const int key = base0 + tile * kKeys + lane_key;
-            if (tile >= n || key < lo || key >= end) return -2;
-            return c.page_table[b * c.table_stride + static_cast<int>(div_by(static_cast<uint32_t>(key), c.page_div))];
+        auto page_in = [&](int tile) KVIO_INLINE {       // of the lane's key; some page for one that no row sees
+            const int key = base0 + tile * kKeys + lane;
+            return c.page_table[b * c.table_stride + static_cast<int>(div_by(static_cast<uint32_t>(key < c.max_ctx ? key : c.max_ctx - 1), c.page_div))];
         };
         float k_scale = 0, v_scale = 0;
-        auto slot_from = [&](int tile, int page) KVIO_INLINE {       // -1 for a key that is not there; asks for its scales
-            const int key = base0 + tile * kKeys + lane_key;
-            const bool there = page >= 0 && page < c.num_pages;
+        uint64_t there_now = 0;                          // the keys that are there
+        int bad_page = -1;
+        auto record_bad = [&]() KVIO_INLINE {
+            if (wave_any(bad_page >= 0) && bad_page >= 0) record_bad_page(c, b, bad_page);
+        };
+        auto slot_from = [&](int tile, int page) KVIO_INLINE {   // 0 for a key that is not there; asks for its scales
+            const int key = base0 + tile * kKeys + lane;
+            const bool seen = tile < n && key >= lo && key < end;
+            const bool there = seen && page >= 0 && page < c.num_pages;
             const int i = static_cast<int>(div_by(static_cast<uint32_t>(key), c.page_div));
-            if (page != -2 && !there) record_bad_page(c, b, i);
+            there_now = wave_ballot(there);
+            bad_page = seen && !there ? i : -1;
             if (E4M3) {
-                k_scale = there ? c.k_scale[page * c.scale_stride + h] * a.scale_log2 : 0.0f;
-                v_scale = there ? c.v_scale[page * c.scale_stride + h] : 0.0f;
+                const int at_page = there ? page : 0;
+                k_scale = c.k_scale[at_page * c.scale_stride + h] * a.scale_log2;
+                v_scale = c.v_scale[at_page * c.scale_stride + h];
             }
-            return there ? page * c.page_size + (key - i * c.page_size) : -1;
+            return there ? page * c.page_size + (key - i * c.page_size) : 0;
         };
-        auto put_scales = [&](int tile) KVIO_INLINE {
-            if (E4M3 && wave == 0) {
-                lds.k_scale[tile & 3][lane] = k_scale;
-                lds.v_scale[tile & 3][lane] = v_scale;
+        auto put_scales = [&](int tile, uint64_t there) KVIO_INLINE {
+            if (E4M3 && wave == 0) {                     // what garbage holds does not count
+                lds.k_scale[tile & 3][lane] = (there >> lane) & 1 ? k_scale : 0.0f;
+                lds.v_scale[tile & 3][lane] = (there >> lane) & 1 ? v_scale : 0.0f;
             }
         };
-        const int piece = tid % S::kPieces, piece_row = tid / S::kPieces;
-        const int64_t cache_row = int64_t(S::kSeg) * c.heads;
-        auto load = [&](u32x4 *x, const uint8_t *cache, int slots) KVIO_INLINE {
-            const uint8_t *p = cache + h * S::kSeg + 16 * piece;
+        const int piece = tid % S::kPieces, piece_row = tid / S::kPieces % kKeys;
+        const uint32_t cache_row = static_cast<uint32_t>(S::kSeg) * static_cast<uint32_t>(c.heads);
+        auto row_slots = [&](uint32_t *slots, int slot) KVIO_INLINE {        // of the thread's rows
 #pragma unroll
-            for (int i = 0; i < S::kPasses; ++i) {
-                const int slot = lane_read(slots, piece_row + i * S::kRowsAtOnce);
-                x[i] = *reinterpret_cast<const u32x4 *>(p + (slot < 0 ? 0 : slot) * cache_row);
+            for (int i = 0; i < S::kPasses; ++i) slots[i] = static_cast<uint32_t>(lane_read(slot, piece_row + i * S::kRowsAtOnce));
+        };
+        const uint8_t *k_from = c.k_cache + h * S::kSeg + 16 * piece, *v_from = c.v_cache + h * S::kSeg + 16 * piece;
+        u32x4 kx[S::kPasses], vx[S::kPasses];
+        auto load_one = [&](const uint8_t *from, uint32_t slot) KVIO_INLINE { return *reinterpret_cast<const u32x4 *>(from + uint64_t(slot) * cache_row); };
+        auto load = [&](u32x4 *x, const uint8_t *from, const uint32_t *slots) KVIO_INLINE {
+#pragma unroll
+            for (int i = 0; i < S::kPasses; ++i) x[i] = load_one(from, slots[i]);
+        };
+        auto put_one = [&](uint8_t *to, int row_bytes, int i, u32x4 x, auto of_v) KVIO_INLINE {
+            uint8_t *w = to + (piece_row + i * S::kRowsAtOnce) * row_bytes + piece * (32 / S::kElem);
+            if constexpr (E4M3) {
+                constexpr bool kBf16 = BF16 || decltype(of_v)::value;         // values meet probabilities
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    *reinterpret_cast<u32x4 *>(w + 16 * e) = u32x4{e4m3_16<kBf16, false>(x[2 * e]), e4m3_16<kBf16, true>(x[2 * e]),
+                                                                   e4m3_16<kBf16, false>(x[2 * e + 1]), e4m3_16<kBf16, true>(x[2 * e + 1])};
+            } else {
+                *reinterpret_cast<u32x4 *>(w) = x;
             }
         };
-        auto put = [&](uint8_t *to, int row_bytes, const u32x4 *x, auto of_v) KVIO_INLINE {
-#pragma unroll
-            for (int i = 0; i < S::kPasses; ++i) {
-                uint8_t *p = to + (piece_row + i * S::kRowsAtOnce) * row_bytes + piece * (32 / S::kElem);
-                if constexpr (E4M3) {
-                    constexpr bool kBf16 = BF16 || decltype(of_v)::value;     // values meet probabilities
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        *reinterpret_cast<u32x4 *>(p + 16 * e) = u32x4{e4m3_16<kBf16, false>(x[i][2 * e]), e4m3_16<kBf16, true>(x[i][2 * e]),
-                                                                       e4m3_16<kBf16, false>(x[i][2 * e + 1]), e4m3_16<kBf16, true>(x[i][2 * e + 1])};
-                } else {
-                    *reinterpret_cast<u32x4 *>(p) = x[i];
-                }
-            }
-        };
-        // Whether all rows of the block see all keys of a tile; `there`: the lanes with a slot.
+        auto put_k = [&](int buffer, int i) KVIO_INLINE { put_one(lds.k[buffer], S::kKRow, i, kx[i], std::false_type()); };
+        auto put_v = [&](int tile, int i) KVIO_INLINE { put_one(lds.v[tile & 1], S::kVRow, i, vx[i], std::true_type()); };
+        // Whether all rows of the block see all keys of a tile.
         auto whole_for_all = [&](int tile, uint64_t there) KVIO_INLINE {
             const int base = base0 + tile * kKeys;
             return base + kKeys - 1 <= first && (a.window == 0 || base > last - a.window) && there == ~0ull;
         };
-        u32x4 kx[S::kPasses], vx[S::kPasses];
-        auto put_k = [&](int buffer) KVIO_INLINE { put(lds.k[buffer], S::kKRow, kx, std::false_type()); };
         // Hidden values may hold anything: those that are not finite become zeros, the tile is marked.
-        auto put_v = [&](int tile, uint64_t there) KVIO_INLINE {
-            if (!whole_for_all(tile, there)) {
-                bool odd = false;
+        auto clean_v = [&](int tile, uint64_t there) KVIO_INLINE {
+            if (whole_for_all(tile, there)) return;
+            bool odd = false;
 #pragma unroll
-                for (int i = 0; i < S::kPasses; ++i) {
-                    const bool is_there = (there >> (piece_row + i * S::kRowsAtOnce)) & 1;
+            for (int i = 0; i < S::kPasses; ++i) {
+                const bool is_there = (there >> (piece_row + i * S::kRowsAtOnce)) & 1;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t v = is_there ? vx[i][e] : 0;
-                        const uint32_t bad = not_finite<BF16, E4M3>(v);
-                        odd = odd || bad != 0;
-                        vx[i][e] = v & ~bad;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t v = is_there ? vx[i][e] : 0;
+                    const uint32_t bad = not_finite<BF16, E4M3>(v);
+                    odd = odd || bad != 0;
+                    vx[i][e] = v & ~bad;
                 }
-                if (odd) lds.odd[(serial + tile) & 3] = serial + tile;
             }
-            put(lds.v[tile & 1], S::kVRow, vx, std::true_type());
+            if (odd) lds.odd[(serial + tile) & 3] = serial + tile;
         };
 
         // ---- products, 32 keys at a time: half i of a tile ---------------------------------
+        // Scores (of keys 8 (e / 4) + 4 g + e % 4) become probabilities, and take part in the maximum, in units of two.
+        constexpr int kUnits = 8 * kColumns, kScoreProducts = S::kSteps * kColumns, kOutProducts = 2 * S::kDimBlocks * kColumns;
         f32x16 score[kColumns], ahead[kColumns];
-        auto scores = [&](int buffer, int i, f32x16 (&x)[kColumns]) KVIO_INLINE {
-            const uint8_t *k = lds.k[buffer] + (32 * i + m) * S::kKRow + 16 * g;
+        u32x4 k_op[S::kKOps], v_op[S::kVOps], p[kColumns][2];
+        f32x4 ks[2], vs[2];                              // e4m3: scales of 4 g + 8 r .. + 3 of a half's keys, of r and r + 1
+        auto fetch_k = [&](int buffer, int i, int e) KVIO_INLINE {
+            k_op[e % S::kKOps] = *reinterpret_cast<const u32x4 *>(lds.k[buffer] + (32 * i + m) * S::kKRow + 16 * g + 32 * e);
+        };
+        auto fetch_v = [&](int tile, int i, int e) KVIO_INLINE {
+            const uint8_t *w = lds.v[tile & 1] + (32 * i + 4 * g + m % 16 / 4) * S::kVRow + 32 * (m / 16) + 8 * (m % 4) +
+                               e / S::kDimBlocks * 16 * S::kVRow + e % S::kDimBlocks * 64;
+            const u32x2 x = lds_turned(w), y = lds_turned(w + 8 * S::kVRow);
+            v_op[e % S::kVOps] = u32x4{x.x, x.y, y.x, y.y};
+        };
+        auto fetch_scales = [&](f32x4 *to, const float *scales, int i, int r) KVIO_INLINE {
+            if constexpr (E4M3) to[r % 2] = *reinterpret_cast<const f32x4 *>(scales + 32 * i + 8 * r + 4 * g);
+        };
+        auto score_product = [&](int i, f32x16 (&x)[kColumns]) KVIO_INLINE {
+            const int e = i / kColumns, t = i % kColumns;
             const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int t = 0; t < kColumns; ++t) x[t] = zero;
-#pragma unroll
-            for (int e = 0; e < S::kSteps; ++e) {
-                const u32x4 op = *reinterpret_cast<const u32x4 *>(k + 32 * e);
-#pragma unroll
-                for (int t = 0; t < kColumns; ++t) x[t] = product32<BF16>(op, q[t][e], x[t]);
-            }
+            x[t] = product32<BF16>(k_op[e % S::kKOps], q[t][e], e == 0 ? zero : x[t]);
         };
-        // Scores by the keys' scales; hidden keys' at minus infinity.
-        auto settle = [&](int tile, int i, uint64_t there, f32x16 (&x)[kColumns]) KVIO_INLINE {
-            const int base = base0 + tile * kKeys + 32 * i;
-            if constexpr (E4M3) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const f32x4 ks = *reinterpret_cast<const f32x4 *>(lds.k_scale[tile & 3] + 32 * i + 8 * r + 4 * g);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int t = 0; t < kColumns; ++t) x[t][4 * r + e] *= ks[e];
-                }
-            }
-            const bool whole = idle || (base + 31 <= wave_first_place && (a.window == 0 || base > wave_last_place - a.window) && there == ~0ull);
-            if (!whole) {
-                const uint32_t mine = static_cast<uint32_t>(there >> (32 * i + 4 * g));
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int at_key = 8 * (e / 4) + e % 4, key = base + at_key + 4 * g;
-                    const bool is_there = (mine >> at_key) & 1;
-#pragma unroll
-                    for (int t = 0; t < kColumns; ++t)
-                        if (!(is_there && key <= place[t] && (a.window == 0 || key > place[t] - a.window))) x[t][e] = kMinusInf;
-                }
-            }
+        auto out_product = [&](int i) KVIO_INLINE {
+            const int e = i / kColumns, t = i % kColumns, u = e / S::kDimBlocks, d = e % S::kDimBlocks;
+            acc[t][d] = product32<S::kPBf16>(v_op[e % S::kVOps], p[t][u], acc[t][d]);
         };
-        // A new maximum where the old one is passed by far.  Scores are in powers of two once multiplied by `unit`.
+        // Scores are in powers of two once multiplied by `unit`.
         const float unit = E4M3 ? 1.0f : a.scale_log2;
-        auto raise = [&](const f32x16 (&x)[kColumns]) KVIO_INLINE {
-            float best[kColumns];
+        float best[kColumns], from[kColumns];            // of a half; what is taken off a score: the maximum, or 0 where there is none
+        auto largest = [&](int i, f32x16 (&x)[kColumns]) KVIO_INLINE {
+            const int t = i % kColumns, e = i / kColumns * 2;
+            if (E4M3) x[t][e] *= ks[e / 4 % 2][e % 4], x[t][e + 1] *= ks[e / 4 % 2][e % 4 + 1];
+            const float of_two = larger(x[t][e], x[t][e + 1]);
+            best[t] = e == 0 ? of_two : larger(best[t], of_two);
+            if (e == 14) keep_here(best[t]);
+        };
+        auto probability = [&](int i, const f32x16 (&x)[kColumns]) KVIO_INLINE {
+            const int t = i % kColumns, e = i / kColumns * 2;
+            float y = exp2_fast(fmaf(x[t][e], unit, -from[t])), z = exp2_fast(fmaf(x[t][e + 1], unit, -from[t]));
+            sum[t] += y + z;
+            if (e == 14) keep_here(sum[t]);
+            if (E4M3) y *= vs[e / 4 % 2][e % 4], z *= vs[e / 4 % 2][e % 4 + 1];
+            p[t][e / 8][e / 2 % 4] = S::kPBf16 ? pack_bf16(y, z) : pack_f16(y, z);
+        };
+        auto mask = [&](int tile, int i, uint64_t there, f32x16 (&x)[kColumns]) KVIO_INLINE { // hidden keys at minus infinity
+            const int base = base0 + tile * kKeys + 32 * i;
+            if (idle || (base + 31 <= wave_first_place && (a.window == 0 || base > wave_last_place - a.window) && there == ~0ull)) return;
+            const uint32_t mine = static_cast<uint32_t>(there >> (32 * i + 4 * g));
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) best[t] = kMinusInf;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at_key = 8 * (e / 4) + e % 4, key = base + at_key + 4 * g;
+                const bool is_there = (mine >> at_key) & 1;
+#pragma unroll
+                for (int t = 0; t < kColumns; ++t) {
+                    if (!(is_there && key <= place[t] && (a.window == 0 || key > place[t] - a.window))) x[t][e] = kMinusInf;
+                    best[t] = larger(best[t], x[t][e]);
+                }
+            }
+        };
+        auto raise = [&]() KVIO_INLINE {                 // a new maximum where the old one is passed by far
             bool any = false;
 #pragma unroll
+            for (int t = 0; t < kColumns; ++t) any = any || best[t] * unit > top[t] + kSlack;
+            if (!wave_any(any)) return;
+#pragma unroll
             for (int t = 0; t < kColumns; ++t) {
-                best[t] = x[t][0];
+                const float mine = best[t] * unit, now = fmaxf(top[t], fmaxf(mine, lane_xor(mine, 32)));
+                const float less = now == kMinusInf ? 1.0f : exp2_fast(top[t] - now);
+                top[t] = now;
+                from[t] = now == kMinusInf ? 0.0f : now;
+                sum[t] *= less;
 #pragma unroll
-                for (int e = 1; e < 16; ++e) best[t] = fmaxf(best[t], x[t][e]);
-                best[t] *= unit;
-                any = any || best[t] > top[t] + kSlack;
+                for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
             }
-            if (wave_any(any)) {
-#pragma unroll
-                for (int t = 0; t < kColumns; ++t) {
-                    const float other = lane_xor(best[t], 32);
-                    const float now = fmaxf(top[t], fmaxf(best[t], other));
-                    const float less = now == kMinusInf ? 1.0f : exp2_fast(top[t] - now);
-                    top[t] = now;
-                    sum[t] *= less;
-#pragma unroll
-                    for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
-                }
-            }
-        };
-        u32x4 p[kColumns][2];
-        auto probabilities = [&](int tile, int i, const f32x16 (&x)[kColumns]) KVIO_INLINE {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f32x4 vs = {1, 1, 1, 1};
-                if (E4M3) vs = *reinterpret_cast<const f32x4 *>(lds.v_scale[tile & 3] + 32 * i + 8 * r + 4 * g);
-#pragma unroll
-                for (int t = 0; t < kColumns; ++t) {
-                    const float from = top[t] == kMinusInf ? 0.0f : top[t];
-                    float e4[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        e4[e] = exp2_fast(fmaf(x[t][4 * r + e], unit, -from));
-                        sum[t] += e4[e];
-                        if (E4M3) e4[e] *= vs[e];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        p[t][r / 2][2 * (r % 2) + e] = S::kPBf16 ? pack_bf16(e4[2 * e], e4[2 * e + 1]) : pack_f16(e4[2 * e], e4[2 * e + 1]);
-                }
-            }
-        };
-        auto outs = [&](int tile, int i) KVIO_INLINE {
-            const uint8_t *v = lds.v[tile & 1] + (32 * i + 4 * g + m % 16 / 4) * S::kVRow + 32 * (m / 16) + 8 * (m % 4);
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int d = 0; d < S::kDimBlocks; ++d) {
-                    const uint8_t *w = v + 16 * u * S::kVRow + 64 * d;
-                    const u32x2 x = lds_turned(w), y = lds_turned(w + 8 * S::kVRow);
-#pragma unroll
-                    for (int t = 0; t < kColumns; ++t) acc[t][d] = product32<S::kPBf16>(u32x4{x.x, x.y, y.x, y.y}, p[t][u], acc[t][d]);
-                }
         };
         // Rare: values that are not finite reach the rows that see them, and no others.
         auto add_odd = [&](int tile) KVIO_INLINE {
@@ -409,68 +408,144 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
         };
 
         // ---- before the first tile ----------------------------------------------------------
-        int slot2, slot3, page4;                         // of tiles j + 2, j + 3, j + 4 in iteration j
+        // In iteration j: the slots of the thread's rows in tiles j + 2 and j + 3, the page of the lane's key in tile
+        // j + 4, the keys that are there in tiles j to j + 3.
+        uint32_t slots2[S::kPasses], slots3[S::kPasses];
+        int page4;
         uint64_t there0, there1, there2, there3;
         {
             const int page0 = page_in(0), page1 = page_in(1), page2 = page_in(2), page3 = page_in(3);
             page4 = page_in(4);
             workgroup_barrier();                         // the block before is done with LDS
             const int slot0 = slot_from(0, page0);
-            load(kx, c.k_cache, slot0);
-            load(vx, c.v_cache, slot0);
-            put_scales(0);
+            record_bad();
+            there0 = there_now;
+            put_scales(0, there0);
+            row_slots(slots2, slot0);
+            load(kx, k_from, slots2);
+            load(vx, v_from, slots2);
             const int slot1 = slot_from(1, page1);
-            put_k(0);
-            load(kx, c.k_cache, slot1);
-            put_scales(1);
-            slot2 = slot_from(2, page2);
-            put_scales(2);
-            slot3 = slot_from(3, page3);
-            there0 = wave_ballot(slot0 >= 0), there1 = wave_ballot(slot1 >= 0);
-            there2 = wave_ballot(slot2 >= 0), there3 = wave_ballot(slot3 >= 0);
-            put_v(0, there0);
-            load(vx, c.v_cache, slot1);
-            put_k(1);
-            load(kx, c.k_cache, slot2);
+            record_bad();
+            there1 = there_now;
+            put_scales(1, there1);
+            row_slots(slots3, slot1);
+#pragma unroll
+            for (int i = 0; i < S::kPasses; ++i) put_k(0, i);
+            load(kx, k_from, slots3);
+            const int slot2 = slot_from(2, page2);
+            record_bad();
+            there2 = there_now;
+            put_scales(2, there2);
+            row_slots(slots2, slot2);
+            clean_v(0, there0);
+#pragma unroll
+            for (int i = 0; i < S::kPasses; ++i) put_v(0, i);
+            load(vx, v_from, slots3);
+            const int slot3 = slot_from(3, page3);
+            record_bad();
+            there3 = there_now;
+            row_slots(slots3, slot3);
+#pragma unroll
+            for (int i = 0; i < S::kPasses; ++i) put_k(1, i);
+            load(kx, k_from, slots2);
             workgroup_barrier();
-            scores(0, 0, score);
-            settle(0, 0, there0, score);
-            raise(score);
+#pragma unroll
+            for (int e = 0; e < S::kKOps; ++e) fetch_k(0, 0, e);
+#pragma unroll
+            for (int i = 0; i < kScoreProducts; ++i) {
+                score_product(i, score);
+                if (i % kColumns == kColumns - 1 && i / kColumns + S::kKOps < S::kSteps) fetch_k(0, 0, i / kColumns + S::kKOps);
+            }
+#pragma unroll
+            for (int e = 0; e < S::kKOps; ++e) fetch_k(0, 1, e);
+            fetch_scales(vs, lds.v_scale[0], 0, 0);
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                if (i % (2 * kColumns) == 0) fetch_scales(ks, lds.k_scale[0], 0, i / (2 * kColumns));
+                largest(i, score);
+            }
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) from[t] = 0;
+            mask(0, 0, there0, score);
+            raise();
         }
-        // ---- tile by tile; what is computed of tiles behind the last one, from no slots, is masked or not used ----
+        // ---- tile by tile; what is computed of tiles behind the last one is masked or not used ----
+        // Each half in two phases: the next half's scores beside this one's probabilities, then this one's part of out^T
+        // beside the next half's maximum.  Operands are fetched, and tiles moved on, one phase or more before they are
+        // used, a little beside each product: a matrix product takes as long as 8 other instructions, and the compiler,
+        // left to itself, puts all of one kind first (8192 tokens of 32 heads, 128 dims: 912 us).
         int k0 = 0;                                      // where K of tile j lies
         for (int j = 0; j < n; ++j) {
-            workgroup_barrier();                         // K of tile j + 1 and V of tile j are there; the buffers of those before free
             const int k1 = k0 + 1 == S::kKBuffers ? 0 : k0 + 1, k2 = k1 + 1 == S::kKBuffers ? 0 : k1 + 1;
-            put_k(k2);
-            put_v(j + 1, there1);
-            put_scales(j + 3);
-            const int slot4 = slot_from(j + 4, page4);
-            page4 = page_in(j + 5);
-            load(vx, c.v_cache, slot2);
-            load(kx, c.k_cache, slot3);
+            workgroup_barrier();                         // K of tile j + 1 and V of tile j are there; the buffers of those before free
+            clean_v(j + 1, there1);
+            put_scales(j + 3, there3);
             in_order();
+            auto scores_phase = [&](int half, const f32x16 (&now)[kColumns], f32x16 (&next)[kColumns]) KVIO_INLINE {
 #pragma unroll
-            for (int i = 0; i < S::kHalves; ++i) {
-                const bool next = i + 1 == S::kHalves;
-                scores(next ? k1 : k0, next ? 0 : i + 1, ahead);
-                probabilities(j, i, score);
-                in_order();
-                outs(j, i);
-                settle(next ? j + 1 : j, next ? 0 : i + 1, next ? there1 : there0, ahead);
-                if (next && lds.odd[(serial + j) & 3] == serial + j) add_odd(j);   // before the maximum moves
-                raise(ahead);
+                for (int i = 0; i < kScoreProducts; ++i) {
+                    score_product(i, next);
+                    in_order();
+                    if (i == kScoreProducts - 1) fetch_scales(ks, lds.k_scale[(j + half) & 3], 1 - half, 0);
+                    if (half == 0 && i < S::kPasses) put_k(k2, i);
+                    if (half == 0 && i >= kScoreProducts - S::kPasses) put_v(j + 1, i - (kScoreProducts - S::kPasses));
 #pragma unroll
-                for (int t = 0; t < kColumns; ++t) score[t] = ahead[t];
-                in_order();
-            }
-            slot2 = slot3, slot3 = slot4;
+                    for (int e = i * S::kVOps / kScoreProducts; e < (i + 1) * S::kVOps / kScoreProducts; ++e) fetch_v(j, half, e);
+                    if (i % kColumns == kColumns - 1 && i / kColumns + S::kKOps < S::kSteps) fetch_k(half == 0 ? k0 : k1, 1 - half, i / kColumns + S::kKOps);
+#pragma unroll
+                    for (int e = i * kUnits / kScoreProducts; e < (i + 1) * kUnits / kScoreProducts; ++e) {
+                        if (e % (2 * kColumns) == 0 && e < 6 * kColumns) fetch_scales(vs, lds.v_scale[j & 3], half, e / (2 * kColumns) + 1);
+                        probability(e, now);
+                    }
+                    in_order();
+                }
+            };
+            auto out_phase = [&](int half, f32x16 (&next)[kColumns]) KVIO_INLINE {
+#pragma unroll
+                for (int i = 0; i < kOutProducts; ++i) {
+                    out_product(i);
+                    in_order();
+                    if (i == kOutProducts - 1) fetch_scales(vs, lds.v_scale[(j + half) & 3], 1 - half, 0);
+                    if (half == 0 && i < S::kPasses) vx[i] = load_one(v_from, slots2[i]);
+                    if (half == 0 && i >= kOutProducts - S::kPasses) kx[i - (kOutProducts - S::kPasses)] = load_one(k_from, slots3[i - (kOutProducts - S::kPasses)]);
+#pragma unroll
+                    for (int e = i * S::kKOps / kOutProducts; e < (i + 1) * S::kKOps / kOutProducts; ++e) fetch_k(k1, half, e);
+                    if (i % kColumns == kColumns - 1 && i / kColumns + S::kVOps < 2 * S::kDimBlocks) fetch_v(j, half, i / kColumns + S::kVOps);
+                    // not beside the first ones: the next scores are just being finished
+                    constexpr int kLate = kOutProducts / 4;
+                    if (i >= kLate)
+#pragma unroll
+                        for (int e = (i - kLate) * kUnits / (kOutProducts - kLate); e < (i + 1 - kLate) * kUnits / (kOutProducts - kLate); ++e) {
+                            if (e % (2 * kColumns) == 0 && e < 6 * kColumns) fetch_scales(ks, lds.k_scale[(j + half) & 3], 1 - half, e / (2 * kColumns) + 1);
+                            largest(e, next);
+                        }
+                    in_order();
+                }
+            };
+            scores_phase(0, score, ahead);
+            out_phase(0, ahead);
+            mask(j, 1, there0, ahead);
+            raise();
+            in_order();
+            scores_phase(1, ahead, score);
+            out_phase(1, score);
+            if (lds.odd[(serial + j) & 3] == serial + j) add_odd(j);   // before the maximum moves
+            mask(j + 1, 0, there1, score);
+            raise();
+            const int slot4 = slot_from(j + 4, page4);
+            record_bad();
+            page4 = page_in(j + 5);
+#pragma unroll
+            for (int i = 0; i < S::kPasses; ++i) slots2[i] = slots3[i];
+            row_slots(slots3, slot4);
             k0 = k1;
-            there0 = there1, there1 = there2, there2 = there3, there3 = wave_ballot(slot4 >= 0);
+            there0 = there1, there1 = there2, there2 = there3, there3 = there_now;
         }
         serial += n;
 
         const bool alone = n == all_tiles;
+        int g8 = 8 * g;                                  // computed here, not kept from block to block
+        keep_here(g8);
 #pragma unroll
         for (int t = 0; t < kColumns; ++t) {
             sum[t] += lane_xor(sum[t], 32);
@@ -487,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
                     for (int r = 0; r < 4; ++r) {
                         const f32x16 &x = acc[t][d];
                         const float x0 = x[4 * r] * inv, x1 = x[4 * r + 1] * inv, x2 = x[4 * r + 2] * inv, x3 = x[4 * r + 3] * inv;
-                        *reinterpret_cast<u32x2 *>(o + 2 * (32 * d + 8 * r + 4 * g)) =
+                        *reinterpret_cast<u32x2 *>(o + 64 * d + 16 * r + g8) =
                             BF16 ? u32x2{pack_bf16(x0, x1), pack_bf16(x2, x3)} : u32x2{pack_f16(x0, x1), pack_f16(x2, x3)};
                     }
                 if (a.lse != nullptr && g == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top[t], sum[t]);
@@ -498,65 +573,71 @@ __global__ void __launch_bounds__(kThreads, 1) attend_blocks(const AttendArgs a)
                 for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + 4 * g) = f32x4{acc[t][d][4 * r], acc[t][d][4 * r + 1], acc[t][d][4 * r + 2], acc[t][d][4 * r + 3]};
+                        *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + g8 / 2) = f32x4{acc[t][d][4 * r], acc[t][d][4 * r + 1], acc[t][d][4 * r + 2], acc[t][d][4 * r + 3]};
                 if (g == 0) *reinterpret_cast<f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row) = f32x2{top[t], sum[t]};
             }
         }
-    }
+    }    if (a.joined && tid == 0) *my_cut = cut;
 }
 
-// Join the partial results of the block that the end of a workgroup's range cuts, by the first workgroup that cuts it.
+// Join the partial results of the block that a workgroup was the first to cut, in order; kJoinRows / 4 rows to a wave.
 template <bool BF16, int D>
-__global__ void __launch_bounds__(kThreads) join_blocks(const AttendArgs a) {
-    constexpr int kDims = D / 64, kKeys = Shape<BF16, false, D>::kKeys;
+__global__ void __launch_bounds__(kJoinThreads) join_blocks(const AttendArgs a) {
+    constexpr int kDims = D / 64, kRows = kJoinRows / kJoinWaves;
     const CacheArgs &c = a.c;
     const int lane = static_cast<int>(threadIdx.x) & 63, wave = wave_first(static_cast<int>(threadIdx.x) >> 6);
     const int parts = (a.slot_rows + kJoinRows - 1) / kJoinRows;
     const int worker = static_cast<int>(blockIdx.x) / parts, part = static_cast<int>(blockIdx.x) - worker * parts;
-    const Line line = line_of(a, lane);
-    const int64_t begin = worker * line.per_worker, cut = begin + line.per_worker;
-    if (cut >= line.all) return;
-    const Where at = where_is(a, line, cut, lane);
-    const Seq s = seq_of(c, at.b);
-    const Blocks blocks = blocks_of(a, s);
-    const int lo = blocks.lo(at.j), hi = blocks.hi(at.j), block_row0 = at.j * a.block_tokens;
-    const int64_t end = at.begin + (hi - lo);
-    auto tile_of = [&](int64_t p) { return static_cast<int>(lo + (p - at.begin)) / kKeys - lo / kKeys; };
-    if (tile_of(cut) == 0) return;                       // not cut after all
-    if (begin > at.begin && tile_of(begin) != 0) return; // cut before
-    const int others = static_cast<int>((end - 1 - cut) / line.per_worker) + 1;      // workgroups behind this one that have a share
+    const Cut cut = reinterpret_cast<const Cut *>(a.partials)[worker];
+    if (cut.others == 0) return;
+    const Seq s = seq_of(c, cut.b);
+    const int block_row0 = cut.j * a.block_tokens, row0 = part * kJoinRows + wave * kRows;
     const int rows = (s.rows - block_row0 < a.block_tokens ? s.rows - block_row0 : a.block_tokens) * a.group;
-    for (int row = part * kJoinRows + wave; row < (part + 1) * kJoinRows && row < rows; row += kWaves) {
-        float top = kMinusInf, sum = 0, acc[kDims] = {};
-        for (int i = 0; i <= others; ++i) {
-            const float *slot = a.partials + block_partial_at(a, worker + i, i == 0 ? 1 : 0, D);
+    if (row0 >= rows) return;
+    float top[kRows], sum[kRows], acc[kRows][kDims];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        top[r] = kMinusInf, sum[r] = 0;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) acc[r][d] = 0;
+    }
+    for (int i = 0; i <= cut.others; ++i) {
+        const float *slot = a.partials + block_partial_at(a, worker + i, i == 0 ? 1 : 0, D);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int row = row0 + r < rows ? row0 + r : rows - 1;
             const f32x2 ends = *reinterpret_cast<const f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row);
             const float *o = slot + int64_t(row) * D;
             const float other = ends.x;
-            const float now = other > top || other != other ? other : top;
-            const float mine = top == kMinusInf || now == top ? 1.0f : exp2_fast(top - now);
+            const float now = other > top[r] || other != other ? other : top[r];
+            const float mine = top[r] == kMinusInf || now == top[r] ? 1.0f : exp2_fast(top[r] - now);
             const float its = other == kMinusInf || now == other ? 1.0f : exp2_fast(other - now);
-            sum = sum * mine + ends.y * its;
+            sum[r] = sum[r] * mine + ends.y * its;
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) acc[d] = acc[d] * mine + o[d * 64 + lane] * its;
-            top = now;
+            for (int d = 0; d < kDims; ++d) acc[r][d] = acc[r][d] * mine + o[d * 64 + lane] * its;
+            top[r] = now;
         }
-        const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div)), qh = at.h * a.group + row - token * a.group;
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int row = row0 + r;
+        if (row >= rows) break;
+        const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div)), qh = cut.h * a.group + row - token * a.group;
         const int64_t array_row = s.row0 + block_row0 + token;
-        const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+        const float inv = sum[r] == 0 ? 0.0f : 1.0f / sum[r];
 #pragma unroll
         for (int d = 0; d < kDims; ++d)
             reinterpret_cast<uint16_t *>(a.out + array_row * a.out_stride + int64_t(qh) * (2 * D))[d * 64 + lane] =
-                static_cast<uint16_t>(BF16 ? pack_bf16(acc[d] * inv, 0) : pack_f16(acc[d] * inv, 0));
-        if (a.lse != nullptr && lane == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top, sum);
+                static_cast<uint16_t>(BF16 ? pack_bf16(acc[r][d] * inv, 0) : pack_f16(acc[r][d] * inv, 0));
+        if (a.lse != nullptr && lane == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top[r], sum[r]);
     }
 }
 
 template <bool BF16, bool E4M3, int D>
 hipError_t launch(const AttendArgs &a, const AttendPlan &plan, hipStream_t stream) {
-    hipLaunchKernelGGL((attend_blocks<BF16, E4M3, D>), dim3(plan.groups), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((attend_blocks<BF16, E4M3, D>), dim3(plan.groups), dim3(64 * waves_of(D)), 0, stream, a);
     if (plan.joined)
-        hipLaunchKernelGGL((join_blocks<BF16, D>), dim3(static_cast<unsigned>((a.workers - 1) * ((a.slot_rows + kJoinRows - 1) / kJoinRows))), dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((join_blocks<BF16, D>), dim3(static_cast<unsigned>((a.workers - 1) * ((a.slot_rows + kJoinRows - 1) / kJoinRows))), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -585,7 +666,7 @@ AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_b
     p.workers = static_cast<int32_t>(p.groups);
     p.joined = workers > 1;
     p.slot_rows = static_cast<int32_t>(std::min<int64_t>(p.block_tokens, max_query) * group + 1) & ~1;
-    if (p.joined) p.bytes = uint64_t(p.workers) * 2 * uint64_t(p.slot_rows) * uint64_t(dim + 2) * 4;
+    if (p.joined) p.bytes = uint64_t(p.workers) * (sizeof(Cut) + 2 * uint64_t(p.slot_rows) * uint64_t(dim + 2) * 4);
     return p;
 }
 

@@ -254,6 +254,7 @@ kvio_status kvio_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *ar
     a.slot_rows = plan.slot_rows;
     a.block_tokens = plan.block_tokens;
     a.min_keys = plan.min_keys;
+    a.joined = plan.joined;
     if (args->workspace_bytes < plan.bytes)
         return fail(KVIO_EINVAL, "%s: workspace of %llu bytes, %llu are needed", fn, (unsigned long long)args->workspace_bytes, (unsigned long long)plan.bytes);
     st = check_array(p, args->workspace, plan.bytes, 16, fn, "workspace");

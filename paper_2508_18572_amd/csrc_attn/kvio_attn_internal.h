@@ -52,6 +52,7 @@ struct AttendArgs {
     float *partials;
     int32_t heads_per_group, workers, min_tiles, slot_rows;
     int32_t block_tokens, min_keys;
+    bool joined;
 };
 
 // How a call of given sizes is split; what it needs of workspace.

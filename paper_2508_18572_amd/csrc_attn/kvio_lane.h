@@ -86,6 +86,8 @@ __device__ __forceinline__ int lane_xor(int v, int mask) { return __shfl_xor(v, 
 __device__ __forceinline__ int lane_up(int v, int by) { return __shfl_up(v, by); }
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float log2_fast(float v) { return __builtin_amdgcn_logf(v); }
+// The larger one; NaN if either is (one instruction, where fmaxf first has to quiet signalling ones).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // Sine and cosine of so many revolutions, up to half of one either way.
 __device__ __forceinline__ f32x2 sin_cos_of(float revolutions) {
     float s, c;
@@ -94,6 +96,9 @@ __device__ __forceinline__ f32x2 sin_cos_of(float revolutions) {
 }
 // The compiler moves nothing past this.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+// v is computed here, not later where it is first used.
+template <class T>
+__device__ __forceinline__ void keep_here(T &v) { asm volatile("" : "+v"(v)); }
 // What lanes of a wave wrote to LDS before is there for its others after.
 __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

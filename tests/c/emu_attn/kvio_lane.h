@@ -154,12 +154,15 @@ inline bool wave_any(bool v) { return wave_ballot(v) != 0; }
 inline int lane_xor(int v, int mask) { return emu_from(v, emu_attn_lane() ^ mask, "lane_xor"); }
 inline int lane_up(int v, int by) { return emu_from(v, emu_attn_lane() < by ? emu_attn_lane() : emu_attn_lane() - by, "lane_up"); }
 inline float exp2_fast(float v) { return exp2f(v); }
+inline float larger(float a, float b) { return a != a ? a : b != b ? b : a > b ? a : b; }
 inline float log2_fast(float v) { return log2f(v); }
 inline f32x2 sin_cos_of(float revolutions) {
     const double t = 6.283185307179586476925 * revolutions;
     return f32x2{static_cast<float>(sin(t)), static_cast<float>(cos(t))};
 }
 inline void in_order() {}
+template <class T>
+void keep_here(T &) {}
 inline void wave_lds_fence() { wave_ballot(true); }
 inline void workgroup_barrier() { emu_attn_barrier(); }
 
