@@ -32,6 +32,9 @@ namespace {
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 constexpr int kJoinRows = 16;                            // rows that a workgroup joins
 
+// Beginning and ending a block takes about as long as so many keys.
+constexpr int kBlockCost = 96;
+
 // The blocks of one sequence and the keys that each goes through.
 struct Blocks {
     int32_t count, first, rows, tokens, window;          // `tokens` to a block
@@ -45,7 +48,7 @@ struct Blocks {
         const int64_t w = int64_t(first) + int64_t(j) * tokens - window + 1;
         return window > 0 && w > 0 ? static_cast<int>(w) : 0;
     }
-    // Keys of all blocks before j, j < count: sums over i < j of hi(i) = max(1, first + (i + 1) tokens) and lo(i).
+    // Length of all blocks before j, j < count: kBlockCost and the keys of each, sums over i < j of hi(i) = max(1, first + (i + 1) tokens) and lo(i).
     __device__ __forceinline__ int64_t before(int j) const {
         const int64_t n = j, z = first < 1 ? std_min(n, (1 - first) / tokens) : 0;
         int64_t sum = z + (n - z) * first + tokens * ((n * (n + 1) - z * (z + 1)) / 2);
@@ -54,9 +57,15 @@ struct Blocks {
             const int64_t y = free < 0 ? 0 : std_min(n, int64_t(static_cast<int>(std_min(free, 0x7fffffff)) / tokens) + 1);
             sum -= (n - y) * (int64_t(first) - window + 1) + tokens * ((n * (n - 1) - y * (y - 1)) / 2);
         }
-        return sum;
+        return sum + n * kBlockCost;
     }
-    __device__ __forceinline__ int64_t keys() const { return count == 0 ? 0 : before(count - 1) + hi(count - 1) - lo(count - 1); }
+    __device__ __forceinline__ int64_t keys() const { return count == 0 ? 0 : before(count - 1) + length(count - 1); }
+    __device__ __forceinline__ int length(int j) const { return kBlockCost + hi(j) - lo(j); }
+    // The tile, counted from the block's first one, that a cut at `at` of its length begins with.
+    __device__ __forceinline__ int tile_at(int j, int64_t at, int keys) const {
+        const int key = lo(j) + (at > kBlockCost ? static_cast<int>(at) - kBlockCost : 0);
+        return key / keys - lo(j) / keys;
+    }
     static __device__ __forceinline__ int64_t std_min(int64_t a, int64_t b) { return a < b ? a : b; }
 };
 __device__ __forceinline__ Blocks blocks_of(const AttendArgs &a, const Seq &s) {
@@ -65,7 +74,7 @@ __device__ __forceinline__ Blocks blocks_of(const AttendArgs &a, const Seq &s) {
 
 // All keys, head after head, sequence after sequence, block after block.
 struct Line {
-    int64_t head, all, per_worker;           // keys of a KV head, of all, of a workgroup
+    int64_t head, all, per_worker;           // length of a KV head, of all, of a workgroup's range
 };
 __device__ __forceinline__ Line line_of(const AttendArgs &a, int lane) {
     int64_t n = 0;
@@ -137,7 +146,7 @@ struct Shape {
     static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 64;
     static constexpr bool kPBf16 = BF16 || E4M3;
     // Operands in registers at a time; with fewer than a phase has, K of a tile is still read while the next but one is put.
-    static constexpr int kKOps = D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 4 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
+    static constexpr int kKOps = D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 3 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
     struct alignas(16) Lds {
         uint8_t k[kKBuffers][kKeys * kKRow], v[2][kKeys * kVRow];
         float k_scale[4][64], v_scale[4][64];            // of tiles, by their number & 3
@@ -178,11 +187,11 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             continue;
         }
         const int lo = blocks.lo(at.j), hi = blocks.hi(at.j), end = blocks.end(at.j);
-        const int64_t next = at.begin + (hi - lo);
+        const int64_t next = at.begin + blocks.length(at.j);
         const int tile0 = lo / kKeys, all_tiles = (hi + kKeys - 1) / kKeys - tile0;
         // A range's end is moved down to a tile's.
-        const int from_tile = pos == at.begin ? 0 : static_cast<int>(lo + (pos - at.begin)) / kKeys - tile0;
-        const int to_tile = stop >= next ? all_tiles : static_cast<int>(lo + (stop - at.begin)) / kKeys - tile0;
+        const int from_tile = blocks.tile_at(at.j, pos - at.begin, kKeys);
+        const int to_tile = stop >= next ? all_tiles : blocks.tile_at(at.j, stop - at.begin, kKeys);
         const int block_row0 = at.j * a.block_tokens;    // in the sequence
         const int n = to_tile - from_tile;
         if (from_tile == 0 && to_tile < all_tiles && to_tile > 0)
@@ -478,8 +487,8 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         for (int j = 0; j < n; ++j) {
             const int k1 = k0 + 1 == S::kKBuffers ? 0 : k0 + 1, k2 = k1 + 1 == S::kKBuffers ? 0 : k1 + 1;
             workgroup_barrier();                         // K of tile j + 1 and V of tile j are there; the buffers of those before free
-            clean_v(j + 1, there1);
             put_scales(j + 3, there3);
+            const int page5 = page_in(j + 5);            // before the tiles' loads, so that waiting for it does not wait for them
             in_order();
             auto scores_phase = [&](int half, const f32x16 (&now)[kColumns], f32x16 (&next)[kColumns]) KVIO_INLINE {
 #pragma unroll
@@ -487,8 +496,10 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                     score_product(i, next);
                     in_order();
                     if (i == kScoreProducts - 1) fetch_scales(ks, lds.k_scale[(j + half) & 3], 1 - half, 0);
-                    if (half == 0 && i < S::kPasses) put_k(k2, i);
-                    if (half == 0 && i >= kScoreProducts - S::kPasses) put_v(j + 1, i - (kScoreProducts - S::kPasses));
+                    if (half == 1 && i < S::kPasses) {
+                        put_k(k2, i);
+                        kx[i] = load_one(k_from, slots3[i]);
+                    }
 #pragma unroll
                     for (int e = i * S::kVOps / kScoreProducts; e < (i + 1) * S::kVOps / kScoreProducts; ++e) fetch_v(j, half, e);
                     if (i % kColumns == kColumns - 1 && i / kColumns + S::kKOps < S::kSteps) fetch_k(half == 0 ? k0 : k1, 1 - half, i / kColumns + S::kKOps);
@@ -506,8 +517,10 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                     out_product(i);
                     in_order();
                     if (i == kOutProducts - 1) fetch_scales(vs, lds.v_scale[(j + half) & 3], 1 - half, 0);
-                    if (half == 0 && i < S::kPasses) vx[i] = load_one(v_from, slots2[i]);
-                    if (half == 0 && i >= kOutProducts - S::kPasses) kx[i - (kOutProducts - S::kPasses)] = load_one(k_from, slots3[i - (kOutProducts - S::kPasses)]);
+                    if (half == 1 && i < S::kPasses) {
+                        put_v(j + 1, i);
+                        vx[i] = load_one(v_from, slots2[i]);
+                    }
 #pragma unroll
                     for (int e = i * S::kKOps / kOutProducts; e < (i + 1) * S::kKOps / kOutProducts; ++e) fetch_k(k1, half, e);
                     if (i % kColumns == kColumns - 1 && i / kColumns + S::kVOps < 2 * S::kDimBlocks) fetch_v(j, half, i / kColumns + S::kVOps);
@@ -527,6 +540,8 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             mask(j, 1, there0, ahead);
             raise();
             in_order();
+            clean_v(j + 1, there1);
+            in_order();
             scores_phase(1, ahead, score);
             out_phase(1, score);
             if (lds.odd[(serial + j) & 3] == serial + j) add_odd(j);   // before the maximum moves
@@ -534,7 +549,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             raise();
             const int slot4 = slot_from(j + 4, page4);
             record_bad();
-            page4 = page_in(j + 5);
+            page4 = page5;
 #pragma unroll
             for (int i = 0; i < S::kPasses; ++i) slots2[i] = slots3[i];
             row_slots(slots3, slot4);
@@ -661,7 +676,7 @@ AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_b
     p.block_tokens = block_rows(dim) / group;
     p.min_keys = 512;                                    // writing and joining a partial result costs as much as some 300 keys
     const int64_t blocks = int64_t(heads) * (b.num_tokens / p.block_tokens + int64_t(b.num_seqs));   // at most
-    const int64_t workers = std::min<int64_t>(256, (blocks * std::max(max_ctx, 1) + p.min_keys - 1) / p.min_keys);   // one to a compute unit
+    const int64_t workers = std::min<int64_t>(256, (blocks * (std::max(max_ctx, 1) + kBlockCost) + p.min_keys - 1) / p.min_keys);   // one to a compute unit
     p.groups = static_cast<uint32_t>((workers + 7) / 8 * 8);
     p.workers = static_cast<int32_t>(p.groups);
     p.joined = workers > 1;
