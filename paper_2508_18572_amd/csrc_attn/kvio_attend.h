@@ -76,6 +76,44 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
     return sum == 0 ? kMinusInf : (top + log2_fast(sum)) * 0.69314718055994530942f;
 }
 
+// Partial results [from, to) of a row, joined by a wave in order: their maximum, sum and sums, D / 64 dims a lane.  Partial
+// i has its D sums at sums(i), its maximum and sum at ends(i).  Four at a time, so that their loads
+// wait for nothing; more cost more in fetching the code than they save (384 partial results of 32 rows: 32 at a time 15 us).
+__device__ __forceinline__ float join_weight(float top, float now) { return top == now || top == kMinusInf ? 1.0f : exp2_fast(top - now); }
+template <int D, class Sums, class Ends>
+__device__ __forceinline__ void join_partials(int from, int to, int lane, Sums sums, Ends ends, float *top, float *sum, float (&acc)[D / 64]) {
+    constexpr int kDims = D / 64, kAtOnce = 4;
+    *top = kMinusInf, *sum = 0;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) acc[d] = 0;
+    for (int i = from; i < to; i += kAtOnce) {
+        float x[kAtOnce][kDims], its_top[kAtOnce], its_sum[kAtOnce];
+        float now = *top;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int at = i + u < to ? i + u : to - 1;
+            const float *o = sums(at), *e = ends(at);
+            its_top[u] = e[0], its_sum[u] = e[1];
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) x[u][d] = o[d * 64 + lane];
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) now = fmaxf(now, its_top[u]);
+        const float mine = join_weight(*top, now);
+        *sum *= mine;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) acc[d] *= mine;
+        *top = now;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const float w = join_weight(its_top[u], now);
+            *sum += i + u < to ? its_sum[u] * w : 0.0f;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) acc[d] += i + u < to ? x[u][d] * w : 0.0f;
+        }
+    }
+}
+
 // Rows of sequences of which no row sees a key: zeros, by one wave for a KV head.
 __device__ __forceinline__ void rows_without_keys(const AttendArgs &a, int h, int lane) {
     for (int b = 0; b < a.c.num_seqs; ++b) {

@@ -30,7 +30,6 @@ namespace kvio {
 namespace {
 
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
-constexpr int kJoinRows = 16;                            // rows that a workgroup joins
 
 // Beginning and ending a block takes about as long as so many keys.
 constexpr int kBlockCost = 96;
@@ -595,56 +594,32 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
     }    if (a.joined && tid == 0) *my_cut = cut;
 }
 
-// Join the partial results of the block that a workgroup was the first to cut, in order; kJoinRows / 4 rows to a wave.
+// Join the partial results of the block that a workgroup was the first to cut, in order, a.join_rows rows to a workgroup.
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kJoinThreads) join_blocks(const AttendArgs a) {
-    constexpr int kDims = D / 64, kRows = kJoinRows / kJoinWaves;
+    constexpr int kDims = D / 64;
     const CacheArgs &c = a.c;
     const int lane = static_cast<int>(threadIdx.x) & 63, wave = wave_first(static_cast<int>(threadIdx.x) >> 6);
-    const int parts = (a.slot_rows + kJoinRows - 1) / kJoinRows;
+    const int parts = (a.slot_rows + a.join_rows - 1) / a.join_rows;
     const int worker = static_cast<int>(blockIdx.x) / parts, part = static_cast<int>(blockIdx.x) - worker * parts;
     const Cut cut = reinterpret_cast<const Cut *>(a.partials)[worker];
     if (cut.others == 0) return;
     const Seq s = seq_of(c, cut.b);
-    const int block_row0 = cut.j * a.block_tokens, row0 = part * kJoinRows + wave * kRows;
+    const int block_row0 = cut.j * a.block_tokens, end = (part + 1) * a.join_rows;
     const int rows = (s.rows - block_row0 < a.block_tokens ? s.rows - block_row0 : a.block_tokens) * a.group;
-    if (row0 >= rows) return;
-    float top[kRows], sum[kRows], acc[kRows][kDims];
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        top[r] = kMinusInf, sum[r] = 0;
-#pragma unroll
-        for (int d = 0; d < kDims; ++d) acc[r][d] = 0;
-    }
-    for (int i = 0; i <= cut.others; ++i) {
-        const float *slot = a.partials + block_partial_at(a, worker + i, i == 0 ? 1 : 0, D);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int row = row0 + r < rows ? row0 + r : rows - 1;
-            const f32x2 ends = *reinterpret_cast<const f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row);
-            const float *o = slot + int64_t(row) * D;
-            const float other = ends.x;
-            const float now = other > top[r] || other != other ? other : top[r];
-            const float mine = top[r] == kMinusInf || now == top[r] ? 1.0f : exp2_fast(top[r] - now);
-            const float its = other == kMinusInf || now == other ? 1.0f : exp2_fast(other - now);
-            sum[r] = sum[r] * mine + ends.y * its;
-#pragma unroll
-            for (int d = 0; d < kDims; ++d) acc[r][d] = acc[r][d] * mine + o[d * 64 + lane] * its;
-            top[r] = now;
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        const int row = row0 + r;
-        if (row >= rows) break;
+    for (int row = part * a.join_rows + wave; row < end && row < rows; row += kJoinWaves) {
+        float top, sum, acc[kDims];
+        auto slot = [&](int i) { return a.partials + block_partial_at(a, worker + i, i == 0 ? 1 : 0, D); };
+        join_partials<D>(0, cut.others + 1, lane, [&](int i) { return slot(i) + int64_t(row) * D; },
+                         [&](int i) { return slot(i) + int64_t(a.slot_rows) * D + 2 * row; }, &top, &sum, acc);
         const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div)), qh = cut.h * a.group + row - token * a.group;
         const int64_t array_row = s.row0 + block_row0 + token;
-        const float inv = sum[r] == 0 ? 0.0f : 1.0f / sum[r];
+        const float inv = sum == 0 ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int d = 0; d < kDims; ++d)
             reinterpret_cast<uint16_t *>(a.out + array_row * a.out_stride + int64_t(qh) * (2 * D))[d * 64 + lane] =
-                static_cast<uint16_t>(BF16 ? pack_bf16(acc[r][d] * inv, 0) : pack_f16(acc[r][d] * inv, 0));
-        if (a.lse != nullptr && lane == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top[r], sum[r]);
+                static_cast<uint16_t>(BF16 ? pack_bf16(acc[d] * inv, 0) : pack_f16(acc[d] * inv, 0));
+        if (a.lse != nullptr && lane == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top, sum);
     }
 }
 
@@ -652,7 +627,7 @@ template <bool BF16, bool E4M3, int D>
 hipError_t launch(const AttendArgs &a, const AttendPlan &plan, hipStream_t stream) {
     hipLaunchKernelGGL((attend_blocks<BF16, E4M3, D>), dim3(plan.groups), dim3(64 * waves_of(D)), 0, stream, a);
     if (plan.joined)
-        hipLaunchKernelGGL((join_blocks<BF16, D>), dim3(static_cast<unsigned>((a.workers - 1) * ((a.slot_rows + kJoinRows - 1) / kJoinRows))), dim3(kJoinThreads), 0, stream, a);
+        hipLaunchKernelGGL((join_blocks<BF16, D>), dim3(static_cast<unsigned>((a.workers - 1) * ((a.slot_rows + a.join_rows - 1) / a.join_rows))), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -680,6 +655,7 @@ AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_b
     p.groups = static_cast<uint32_t>((workers + 7) / 8 * 8);
     p.workers = static_cast<int32_t>(p.groups);
     p.joined = workers > 1;
+    p.join_rows = blocks <= 64 ? 4 : 16;                 // few blocks have many partial results each
     p.slot_rows = static_cast<int32_t>(std::min<int64_t>(p.block_tokens, max_query) * group + 1) & ~1;
     if (p.joined) p.bytes = uint64_t(p.workers) * (sizeof(Cut) + 2 * uint64_t(p.slot_rows) * uint64_t(dim + 2) * 4);
     return p;

@@ -25,6 +25,7 @@ namespace kvio {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kFewRows = 512;                  // rows and query heads, below which each is joined by 16 waves
 
 // A wave's slots and scales of two tiles, and its rows of Q.
 template <int D, int NT>
@@ -332,14 +333,17 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
     }
 }
 
-// Join the partial results of one row, in order: a wave for each, D / 64 dims a lane.
-template <bool BF16, int D>
-__global__ void __launch_bounds__(kThreads) join_steps(const AttendArgs a) {
+// Join the partial results of a row and query head: a wave's work, or, where few rows have many partial results each,
+// a workgroup's, each wave a run of them, then the first the waves'.
+template <bool BF16, int D, int WAVES>
+__global__ void __launch_bounds__(WAVES > 1 ? 64 * WAVES : kThreads) join_steps(const AttendArgs a) {
     constexpr int kDims = D / 64;
-    __shared__ float shared[kWaves][D + 2];
+    __shared__ float shared[WAVES][D + 2];
     const CacheArgs &c = a.c;
     const int lane = static_cast<int>(threadIdx.x) & 63, wave = wave_first(static_cast<int>(threadIdx.x) >> 6);
-    const int row = static_cast<int>(blockIdx.x) / a.q_heads, qh = static_cast<int>(blockIdx.x) - row * a.q_heads;
+    const int at = WAVES > 1 ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) * kWaves + wave;
+    const int row = at / a.q_heads, qh = at - row * a.q_heads;
+    if (row >= c.num_tokens) return;
     const int b = seq_with_row(c, row, lane);
     if (b < 0) return;
     const Seq s = seq_of(c, b);
@@ -348,29 +352,24 @@ __global__ void __launch_bounds__(kThreads) join_steps(const AttendArgs a) {
     const Ranges r = ranges_of(a, lane, b, &begin);
     const int tiles = span_of(a, s).tiles;
     if (tiles == 0) return;
-    const int64_t w0 = begin / r.per_worker, w1 = (begin + tiles - 1) / r.per_worker;
+    const int w0 = static_cast<int>(begin / r.per_worker), w1 = static_cast<int>((begin + tiles - 1) / r.per_worker);
     if (w0 == w1) return;
     const int h = qh / a.group, at_row = (row - s.row0) * a.group + qh - h * a.group;
-    // Each wave joins a run of them, then the first joins the waves'.
-    const int64_t n = w1 - w0 + 1, share = (n + kWaves - 1) / kWaves;
-    float top = kMinusInf, sum = 0, acc[kDims] = {};
-    auto take = [&](const float *o) {
-        const float other = o[D], other_sum = o[D + 1];
-        const float now = other > top || other != other ? other : top;
-        const float mine = top == kMinusInf || now == top ? 1.0f : exp2_fast(top - now);
-        const float its = other == kMinusInf || now == other ? 1.0f : exp2_fast(other - now);
-        sum = sum * mine + other_sum * its;
-        for (int d = 0; d < kDims; ++d) acc[d] = acc[d] * mine + o[d * 64 + lane] * its;
-        top = now;
-    };
-    for (int64_t w = w0 + wave * share; w < w0 + (wave + 1) * share && w <= w1; ++w)
-        take(a.partials + partial_at(a, static_cast<int>(w), h, w == w0 ? 1 : 0, at_row, D));
-    if (lane == 0) shared[wave][D] = top, shared[wave][D + 1] = sum;
-    for (int d = 0; d < kDims; ++d) shared[wave][d * 64 + lane] = acc[d];
-    workgroup_barrier();
-    if (wave != 0) return;
-    for (int w = 1; w < kWaves; ++w) take(shared[w]);
+    const int n = w1 - w0 + 1, share = (n + WAVES - 1) / WAVES;
+    float top, sum, acc[kDims];
+    auto sums = [&](int i) { return a.partials + partial_at(a, w0 + i, h, i == 0 ? 1 : 0, at_row, D); };
+    const int from = WAVES > 1 ? wave * share : 0;
+    join_partials<D>(from, from + share < n ? from + share : n, lane, sums, [&](int i) { return sums(i) + D; }, &top, &sum, acc);
+    if constexpr (WAVES > 1) {
+        if (lane == 0) shared[wave][D] = top, shared[wave][D + 1] = sum;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) shared[wave][d * 64 + lane] = acc[d];
+        workgroup_barrier();
+        if (wave != 0) return;
+        join_partials<D>(0, (n + share - 1) / share, lane, [&](int i) { return shared[i]; }, [&](int i) { return shared[i] + D; }, &top, &sum, acc);
+    }
     const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+#pragma unroll
     for (int d = 0; d < kDims; ++d)
         reinterpret_cast<uint16_t *>(a.out + row * a.out_stride + int64_t(qh) * (2 * D))[d * 64 + lane] =
             static_cast<uint16_t>(BF16 ? pack_bf16(acc[d] * inv, 0) : pack_f16(acc[d] * inv, 0));
@@ -381,8 +380,15 @@ template <bool BF16, bool E4M3, int D>
 hipError_t launch(const AttendArgs &a, const AttendPlan &plan, hipStream_t stream) {
     if (plan.columns == 1) hipLaunchKernelGGL((attend_steps<BF16, E4M3, D, 1>), dim3(plan.groups), dim3(kThreads), 0, stream, a);
     else if (plan.columns == 2) hipLaunchKernelGGL((attend_steps<BF16, E4M3, D, 2>), dim3(plan.groups), dim3(kThreads), 0, stream, a);
-    else if constexpr (D <= 128) hipLaunchKernelGGL((attend_steps<BF16, E4M3, D, 4>), dim3(plan.groups), dim3(kThreads), 0, stream, a);
-    if (plan.joined) hipLaunchKernelGGL((join_steps<BF16, D>), dim3(static_cast<unsigned>(a.c.num_tokens) * static_cast<unsigned>(a.q_heads)), dim3(kThreads), 0, stream, a);
+    else if constexpr (D <= 128) {
+        if (plan.columns == 3) hipLaunchKernelGGL((attend_steps<BF16, E4M3, D, 3>), dim3(plan.groups), dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((attend_steps<BF16, E4M3, D, 4>), dim3(plan.groups), dim3(kThreads), 0, stream, a);
+    }
+    const int64_t rows = int64_t(a.c.num_tokens) * a.q_heads;
+    if (plan.joined && rows <= kFewRows)
+        hipLaunchKernelGGL((join_steps<BF16, D, 16>), dim3(static_cast<unsigned>(rows)), dim3(1024), 0, stream, a);
+    else if (plan.joined)
+        hipLaunchKernelGGL((join_steps<BF16, D, 1>), dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -404,7 +410,7 @@ AttendPlan plan_steps(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, co
     AttendPlan p = {};
     const int64_t rows = int64_t(max_query) * (q_heads / heads);
     p.few = true;
-    p.columns = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.columns = static_cast<int32_t>((rows + 15) / 16);
     p.heads_per_group = heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1;
     const int64_t head_groups = heads / p.heads_per_group, splits = kWaves / p.heads_per_group;
     // As many workgroups as the GPU holds at once: 256 compute units, a wave on each SIMD for each of them.

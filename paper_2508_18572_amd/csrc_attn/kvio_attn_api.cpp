@@ -121,6 +121,9 @@ kvio_status check_cache(kvio_pool_t p, int32_t layer, const kvio_batch &b, bool 
     return KVIO_OK;
 }
 
+// Rows of a KV head that kvio_attend_steps.hip holds in a wave's registers, by the size of heads.
+int64_t most_step_rows(int64_t dim) { return dim <= 128 ? 64 : 32; }
+
 kvio_status check_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *args, const char *fn) {
     if (args == nullptr) return fail(KVIO_EINVAL, "%s: null arguments", fn);
     const kvio_status st = check_sizes(p, layer, args->batch, args->dtype, args->cache_dtype, fn);
@@ -138,13 +141,12 @@ kvio_status check_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *a
     const int64_t tiles = (int64_t(args->batch.max_pages) * p->g.page_size + 63) / 32;
     if (args->batch.num_seqs > 0 && args->batch.num_tokens > 0 && tiles * args->batch.num_seqs > INT32_MAX - 4096)
         return fail(KVIO_EINVAL, "%s: %d contexts of up to %d pages: too many tokens to count", fn, args->batch.num_seqs, args->batch.max_pages);
-    if (int64_t(args->batch.num_tokens) * args->num_q_heads > INT32_MAX)
+    // a wave for each when partial results are joined, and fewer than 2^32 threads to a launch
+    const bool few = int64_t(longest_query(args->batch)) * group <= most_step_rows(dim);
+    if (int64_t(args->batch.num_tokens) * args->num_q_heads > (few ? (1 << 26) - 4 : INT32_MAX))
         return fail(KVIO_EINVAL, "%s: %d tokens of %d heads: too many rows to count", fn, args->batch.num_tokens, args->num_q_heads);
     return KVIO_OK;
 }
-
-// Rows of a KV head that kvio_attend_steps.hip holds in a wave's registers, by the size of heads.
-int64_t most_step_rows(int64_t dim) { return dim <= 128 ? 64 : 32; }
 
 kvio::AttendPlan plan_of(kvio_pool_t p, const kvio_attend_args &args) {
     const kvio::PoolGeom &g = p->g;
@@ -203,6 +205,7 @@ kvio_status kvio_append(kvio_pool_t p, int32_t layer, const kvio_append_args *ar
     a.rot_half = args->rot_dim / 2;
     a.interleaved = (args->flags & KVIO_APPEND_INTERLEAVED) != 0;
     a.page_items = static_cast<int32_t>(std::min(N, N / p->g.page_size + 2 * int64_t(b.num_seqs)));
+    if (kvio::append_threads(a, e4m3) >= int64_t(1) << 32) return fail(KVIO_EINVAL, "%s: %lld tokens are too many for one call", fn, (long long)N);
     const hipError_t e = kvio::launch_append(a, args->dtype, e4m3, stream);
     return e == hipSuccess ? KVIO_OK : kvio::fail_hip(e, fn);
 }
@@ -255,6 +258,7 @@ kvio_status kvio_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *ar
     a.block_tokens = plan.block_tokens;
     a.min_keys = plan.min_keys;
     a.joined = plan.joined;
+    a.join_rows = plan.join_rows;
     if (args->workspace_bytes < plan.bytes)
         return fail(KVIO_EINVAL, "%s: workspace of %llu bytes, %llu are needed", fn, (unsigned long long)args->workspace_bytes, (unsigned long long)plan.bytes);
     st = check_array(p, args->workspace, plan.bytes, 16, fn, "workspace");

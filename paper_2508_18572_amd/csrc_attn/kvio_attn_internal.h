@@ -51,7 +51,7 @@ struct AttendArgs {
     // How the work is split (AttendPlan).
     float *partials;
     int32_t heads_per_group, workers, min_tiles, slot_rows;
-    int32_t block_tokens, min_keys;
+    int32_t block_tokens, min_keys, join_rows;
     bool joined;
 };
 
@@ -60,7 +60,7 @@ struct AttendPlan {
     bool few;                      // few rows to a sequence: kvio_attend_steps.hip, else kvio_attend_blocks.hip
     int32_t columns;               // blocks of 16 rows that a wave holds
     int32_t heads_per_group, workers, min_tiles, slot_rows;
-    int32_t block_tokens, min_keys;
+    int32_t block_tokens, min_keys, join_rows;
     uint32_t groups;               // workgroups
     bool joined;                   // partial results may be left
     uint64_t bytes;
@@ -70,6 +70,7 @@ constexpr int block_rows(int dim) { return dim <= 128 ? 256 : 128; }
 AttendPlan plan_steps(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
 AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
 
+int64_t append_threads(const AppendArgs &a, bool e4m3);      // that launch_append starts; fewer than 2^32 can be
 hipError_t launch_append(const AppendArgs &a, int32_t dtype, bool e4m3, hipStream_t stream);
 hipError_t launch_steps(const AttendArgs &a, const AttendPlan &plan, int32_t dtype, bool e4m3, hipStream_t stream);
 hipError_t launch_blocks(const AttendArgs &a, const AttendPlan &plan, int32_t dtype, bool e4m3, hipStream_t stream);
