@@ -126,7 +126,7 @@ def _on(pool, stream, call):
     """Run call(raw stream) with `stream` and the pool's GPU current."""
     dev = pool.tensor.device
     if stream is None and dev.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream)
+        return call(torch._C._cuda_getCurrentRawStream(dev.index))   # current_stream() takes microseconds
     with torch.cuda.device(dev):
         s = torch.cuda.current_stream() if stream is None else stream
         if isinstance(s, int):

@@ -128,6 +128,25 @@ __device__ __forceinline__ void rows_without_keys(const AttendArgs &a, int h, in
     }
 }
 
+// fp16 probabilities meet e4m3 values with their scales in units of a power of two that follows the largest scale so far:
+// products with probabilities (up to 2^8) stay below 2^15, and far smaller scales keep their precision.  Of a wave; out^T is
+// kept in that unit.
+struct ValueUnit {
+    float unit = 0x1p-120f, inverse = 0x1p120f;
+    // `scale`: of the lane's key (0 for none).  What out^T has to be multiplied by.
+    __device__ __forceinline__ float take(float scale) {
+        const float size = fabsf(scale);
+        if (!wave_any(size > 128 * unit)) return 1.0f;
+        float most = size <= 0x1p120f ? size : 0.0f;
+        for (int by = 1; by < 64; by *= 2) most = fmaxf(most, lane_xor(most, by));
+        if (!(most > 128 * unit)) return 1.0f;
+        const float before = unit;
+        unit = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, most) & 0x7f800000u)) * 0x1p-6f;
+        inverse = 1.0f / unit;
+        return before * inverse;
+    }
+};
+
 // Ones where an element of the word, two of 16 bits or four codes, is infinite or NaN.
 template <bool BF16, bool E4M3>
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {

@@ -21,7 +21,6 @@
 #include "kvio_attend.h"
 
 #include <algorithm>
-#include <type_traits>
 
 // Registers that lambdas work on stay registers only where the calls are gone early.
 #define KVIO_INLINE __attribute__((always_inline))
@@ -143,7 +142,7 @@ struct Shape {
     static constexpr int kPieces = kSeg / 16, kRowsAtOnce = std::min(kKeys, kThreads / kPieces), kPasses = kKeys / kRowsAtOnce;
     // 16 rows' pieces of 16 bytes lie in all banks; so do 32 bytes of 8 rows
     static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 64;
-    static constexpr bool kPBf16 = BF16 || E4M3;
+    static constexpr bool kUnit = E4M3 && !BF16;         // ValueUnit
     // Operands in registers at a time; with fewer than a phase has, K of a tile is still read while the next but one is put.
     static constexpr int kKOps = D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 3 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
     struct alignas(16) Lds {
@@ -238,6 +237,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             return c.page_table[b * c.table_stride + static_cast<int>(div_by(static_cast<uint32_t>(key < c.max_ctx ? key : c.max_ctx - 1), c.page_div))];
         };
         float k_scale = 0, v_scale = 0;
+        ValueUnit value_unit;
         uint64_t there_now = 0;                          // the keys that are there
         int bad_page = -1;
         auto record_bad = [&]() KVIO_INLINE {
@@ -258,6 +258,14 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             return there ? page * c.page_size + (key - i * c.page_size) : 0;
         };
         auto put_scales = [&](int tile, uint64_t there) KVIO_INLINE {
+            if constexpr (S::kUnit) {                    // long before the tile is worked on
+                const float less = value_unit.take((there >> lane) & 1 ? v_scale : 0.0f);
+                if (less != 1.0f)
+#pragma unroll
+                    for (int t = 0; t < kColumns; ++t)
+#pragma unroll
+                        for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
+            }
             if (E4M3 && wave == 0) {                     // what garbage holds does not count
                 lds.k_scale[tile & 3][lane] = (there >> lane) & 1 ? k_scale : 0.0f;
                 lds.v_scale[tile & 3][lane] = (there >> lane) & 1 ? v_scale : 0.0f;
@@ -276,20 +284,19 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
 #pragma unroll
             for (int i = 0; i < S::kPasses; ++i) x[i] = load_one(from, slots[i]);
         };
-        auto put_one = [&](uint8_t *to, int row_bytes, int i, u32x4 x, auto of_v) KVIO_INLINE {
+        auto put_one = [&](uint8_t *to, int row_bytes, int i, u32x4 x) KVIO_INLINE {
             uint8_t *w = to + (piece_row + i * S::kRowsAtOnce) * row_bytes + piece * (32 / S::kElem);
             if constexpr (E4M3) {
-                constexpr bool kBf16 = BF16 || decltype(of_v)::value;         // values meet probabilities
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    *reinterpret_cast<u32x4 *>(w + 16 * e) = u32x4{e4m3_16<kBf16, false>(x[2 * e]), e4m3_16<kBf16, true>(x[2 * e]),
-                                                                   e4m3_16<kBf16, false>(x[2 * e + 1]), e4m3_16<kBf16, true>(x[2 * e + 1])};
+                    *reinterpret_cast<u32x4 *>(w + 16 * e) = u32x4{e4m3_16<BF16, false>(x[2 * e]), e4m3_16<BF16, true>(x[2 * e]),
+                                                                   e4m3_16<BF16, false>(x[2 * e + 1]), e4m3_16<BF16, true>(x[2 * e + 1])};
             } else {
                 *reinterpret_cast<u32x4 *>(w) = x;
             }
         };
-        auto put_k = [&](int buffer, int i) KVIO_INLINE { put_one(lds.k[buffer], S::kKRow, i, kx[i], std::false_type()); };
-        auto put_v = [&](int tile, int i) KVIO_INLINE { put_one(lds.v[tile & 1], S::kVRow, i, vx[i], std::true_type()); };
+        auto put_k = [&](int buffer, int i) KVIO_INLINE { put_one(lds.k[buffer], S::kKRow, i, kx[i]); };
+        auto put_v = [&](int tile, int i) KVIO_INLINE { put_one(lds.v[tile & 1], S::kVRow, i, vx[i]); };
         // Whether all rows of the block see all keys of a tile.
         auto whole_for_all = [&](int tile, uint64_t there) KVIO_INLINE {
             const int base = base0 + tile * kKeys;
@@ -338,7 +345,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         };
         auto out_product = [&](int i) KVIO_INLINE {
             const int e = i / kColumns, t = i % kColumns, u = e / S::kDimBlocks, d = e % S::kDimBlocks;
-            acc[t][d] = product32<S::kPBf16>(v_op[e % S::kVOps], p[t][u], acc[t][d]);
+            acc[t][d] = product32<BF16>(v_op[e % S::kVOps], p[t][u], acc[t][d]);
         };
         // Scores are in powers of two once multiplied by `unit`.
         const float unit = E4M3 ? 1.0f : a.scale_log2;
@@ -355,8 +362,9 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             float y = exp2_fast(fmaf(x[t][e], unit, -from[t])), z = exp2_fast(fmaf(x[t][e + 1], unit, -from[t]));
             sum[t] += y + z;
             if (e == 14) keep_here(sum[t]);
+            if (S::kUnit) y *= value_unit.inverse, z *= value_unit.inverse;
             if (E4M3) y *= vs[e / 4 % 2][e % 4], z *= vs[e / 4 % 2][e % 4 + 1];
-            p[t][e / 8][e / 2 % 4] = S::kPBf16 ? pack_bf16(y, z) : pack_f16(y, z);
+            p[t][e / 8][e / 2 % 4] = BF16 ? pack_bf16(y, z) : pack_f16(y, z);
         };
         auto mask = [&](int tile, int i, uint64_t there, f32x16 (&x)[kColumns]) KVIO_INLINE { // hidden keys at minus infinity
             const int base = base0 + tile * kKeys + 32 * i;
@@ -567,7 +575,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             if (row >= rows) continue;
             if (alone) {
                 const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div)), qh = h * a.group + row - token * a.group;
-                const float inv = sum[t] == 0 ? 0.0f : 1.0f / sum[t];
+                const float inv = sum[t] == 0 ? 0.0f : (S::kUnit ? value_unit.unit : 1.0f) / sum[t];
                 const int64_t array_row = s.row0 + block_row0 + token;
                 uint8_t *o = a.out + array_row * a.out_stride + int64_t(qh) * (2 * D);
 #pragma unroll
@@ -583,11 +591,12 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             } else {
                 float *slot = a.partials + block_partial_at(a, worker, from_tile != 0 ? 0 : 1, D);
                 float *o = slot + int64_t(row) * D;
+                const float by = S::kUnit ? value_unit.unit : 1.0f;
 #pragma unroll
                 for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + g8 / 2) = f32x4{acc[t][d][4 * r], acc[t][d][4 * r + 1], acc[t][d][4 * r + 2], acc[t][d][4 * r + 3]};
+                        *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + g8 / 2) = f32x4{acc[t][d][4 * r] * by, acc[t][d][4 * r + 1] * by, acc[t][d][4 * r + 2] * by, acc[t][d][4 * r + 3] * by};
                 if (g == 0) *reinterpret_cast<f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row) = f32x2{top[t], sum[t]};
             }
         }
