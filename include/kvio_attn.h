@@ -99,9 +99,9 @@ kvio_status kvio_append(kvio_pool_t pool, int32_t layer, const kvio_append_args 
  * window > 0, the last `window` of those only.  A row that sees no token gets zeros and an lse
  * of minus infinity; lse[row][h] (if not NULL) is the natural logarithm of the softmax's sum.
  * What hidden tokens hold, infinities and NaN included, has no effect.
- * Products are accumulated in fp32, probabilities rounded to `dtype` for the
- * second one (with an e4m3 cache, times their values' scales; in fp16 these lose precision below
- * 2^-18 of the largest scale of the context).  Equal inputs give equal bits, except over other max_pages, max_query or GPUs.
+ * Products are accumulated in fp32, probabilities rounded to the cache's type for the second one; with an
+ * e4m3 cache to fp16, times their values' scales (a scale below 2^-18 of the context's largest loses precision).
+ * Equal inputs give equal bits, except over other max_pages, max_query or GPUs.
  * Rows of no sequence are left alone. */
 typedef struct kvio_attend_args {
     kvio_batch batch;

@@ -128,7 +128,7 @@ __device__ __forceinline__ void rows_without_keys(const AttendArgs &a, int h, in
     }
 }
 
-// fp16 probabilities meet e4m3 values with their scales in units of a power of two that follows the largest scale so far:
+// fp16 probabilities meet e4m3 values with these' scales, in units of a power of two that follows the largest scale so far:
 // products with probabilities (up to 2^8) stay below 2^15, and far smaller scales keep their precision.  Of a wave; out^T is
 // kept in that unit.
 struct ValueUnit {

@@ -21,6 +21,7 @@
 #include "kvio_attend.h"
 
 #include <algorithm>
+#include <type_traits>
 
 // Registers that lambdas work on stay registers only where the calls are gone early.
 #define KVIO_INLINE __attribute__((always_inline))
@@ -142,7 +143,7 @@ struct Shape {
     static constexpr int kPieces = kSeg / 16, kRowsAtOnce = std::min(kKeys, kThreads / kPieces), kPasses = kKeys / kRowsAtOnce;
     // 16 rows' pieces of 16 bytes lie in all banks; so do 32 bytes of 8 rows
     static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 64;
-    static constexpr bool kUnit = E4M3 && !BF16;         // ValueUnit
+    static constexpr bool kPBf16 = BF16 && !E4M3;        // probabilities' and values' type: fp16, in a ValueUnit, for e4m3 values
     // Operands in registers at a time; with fewer than a phase has, K of a tile is still read while the next but one is put.
     static constexpr int kKOps = D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 3 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
     struct alignas(16) Lds {
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             return there ? page * c.page_size + (key - i * c.page_size) : 0;
         };
         auto put_scales = [&](int tile, uint64_t there) KVIO_INLINE {
-            if constexpr (S::kUnit) {                    // long before the tile is worked on
+            if constexpr (E4M3) {                    // long before the tile is worked on
                 const float less = value_unit.take((there >> lane) & 1 ? v_scale : 0.0f);
                 if (less != 1.0f)
 #pragma unroll
@@ -284,19 +285,20 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
 #pragma unroll
             for (int i = 0; i < S::kPasses; ++i) x[i] = load_one(from, slots[i]);
         };
-        auto put_one = [&](uint8_t *to, int row_bytes, int i, u32x4 x) KVIO_INLINE {
+        auto put_one = [&](uint8_t *to, int row_bytes, int i, u32x4 x, auto as_bf16) KVIO_INLINE {
             uint8_t *w = to + (piece_row + i * S::kRowsAtOnce) * row_bytes + piece * (32 / S::kElem);
             if constexpr (E4M3) {
+                constexpr bool kBf16 = decltype(as_bf16)::value;
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    *reinterpret_cast<u32x4 *>(w + 16 * e) = u32x4{e4m3_16<BF16, false>(x[2 * e]), e4m3_16<BF16, true>(x[2 * e]),
-                                                                   e4m3_16<BF16, false>(x[2 * e + 1]), e4m3_16<BF16, true>(x[2 * e + 1])};
+                    *reinterpret_cast<u32x4 *>(w + 16 * e) = u32x4{e4m3_16<kBf16, false>(x[2 * e]), e4m3_16<kBf16, true>(x[2 * e]),
+                                                                   e4m3_16<kBf16, false>(x[2 * e + 1]), e4m3_16<kBf16, true>(x[2 * e + 1])};
             } else {
                 *reinterpret_cast<u32x4 *>(w) = x;
             }
         };
-        auto put_k = [&](int buffer, int i) KVIO_INLINE { put_one(lds.k[buffer], S::kKRow, i, kx[i]); };
-        auto put_v = [&](int tile, int i) KVIO_INLINE { put_one(lds.v[tile & 1], S::kVRow, i, vx[i]); };
+        auto put_k = [&](int buffer, int i) KVIO_INLINE { put_one(lds.k[buffer], S::kKRow, i, kx[i], std::bool_constant<BF16>()); };
+        auto put_v = [&](int tile, int i) KVIO_INLINE { put_one(lds.v[tile & 1], S::kVRow, i, vx[i], std::bool_constant<S::kPBf16>()); };
         // Whether all rows of the block see all keys of a tile.
         auto whole_for_all = [&](int tile, uint64_t there) KVIO_INLINE {
             const int base = base0 + tile * kKeys;
@@ -345,7 +347,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         };
         auto out_product = [&](int i) KVIO_INLINE {
             const int e = i / kColumns, t = i % kColumns, u = e / S::kDimBlocks, d = e % S::kDimBlocks;
-            acc[t][d] = product32<BF16>(v_op[e % S::kVOps], p[t][u], acc[t][d]);
+            acc[t][d] = product32<S::kPBf16>(v_op[e % S::kVOps], p[t][u], acc[t][d]);
         };
         // Scores are in powers of two once multiplied by `unit`.
         const float unit = E4M3 ? 1.0f : a.scale_log2;
@@ -362,9 +364,9 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             float y = exp2_fast(fmaf(x[t][e], unit, -from[t])), z = exp2_fast(fmaf(x[t][e + 1], unit, -from[t]));
             sum[t] += y + z;
             if (e == 14) keep_here(sum[t]);
-            if (S::kUnit) y *= value_unit.inverse, z *= value_unit.inverse;
+            if (E4M3) y *= value_unit.inverse, z *= value_unit.inverse;
             if (E4M3) y *= vs[e / 4 % 2][e % 4], z *= vs[e / 4 % 2][e % 4 + 1];
-            p[t][e / 8][e / 2 % 4] = BF16 ? pack_bf16(y, z) : pack_f16(y, z);
+            p[t][e / 8][e / 2 % 4] = S::kPBf16 ? pack_bf16(y, z) : pack_f16(y, z);
         };
         auto mask = [&](int tile, int i, uint64_t there, f32x16 (&x)[kColumns]) KVIO_INLINE { // hidden keys at minus infinity
             const int base = base0 + tile * kKeys + 32 * i;
@@ -575,7 +577,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             if (row >= rows) continue;
             if (alone) {
                 const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div)), qh = h * a.group + row - token * a.group;
-                const float inv = sum[t] == 0 ? 0.0f : (S::kUnit ? value_unit.unit : 1.0f) / sum[t];
+                const float inv = sum[t] == 0 ? 0.0f : (E4M3 ? value_unit.unit : 1.0f) / sum[t];
                 const int64_t array_row = s.row0 + block_row0 + token;
                 uint8_t *o = a.out + array_row * a.out_stride + int64_t(qh) * (2 * D);
 #pragma unroll
@@ -591,7 +593,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             } else {
                 float *slot = a.partials + block_partial_at(a, worker, from_tile != 0 ? 0 : 1, D);
                 float *o = slot + int64_t(row) * D;
-                const float by = S::kUnit ? value_unit.unit : 1.0f;
+                const float by = E4M3 ? value_unit.unit : 1.0f;
 #pragma unroll
                 for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll

@@ -47,8 +47,9 @@ struct Steps {
     static constexpr int kSteps = D / 32;                // products along a head
     static constexpr int kKWords = D * kElem / 16;       // words of K to a lane and 16 keys
     static constexpr int kVWords = kDims * kElem / 4;    // words of V to a lane and key
-    // Probabilities take the queries' type.  With e4m3 values they carry these' scales; bf16 has the range for that.
-    static constexpr bool kUnit = E4M3 && !BF16;
+    // Probabilities take the cache's type; beside e4m3 values, whose scales they carry, fp16 (in bf16 their roundings were
+    // the larger part of the result's error) in a ValueUnit.
+    static constexpr bool kPBf16 = BF16 && !E4M3;
 
     struct Tile {
         uint32_t k[2][kKWords];
@@ -100,10 +101,10 @@ struct Steps {
             const uint32_t x = t.v[2 * p][w], y = t.v[2 * p + 1][w];
             if constexpr (E4M3) {
                 const uint32_t a = bytes_of(y, x, 0x05010400), b = bytes_of(y, x, 0x07030602);
-                out[0][p] = e4m3_16<BF16, false>(a);
-                out[1][p] = e4m3_16<BF16, true>(a);
-                out[2][p] = e4m3_16<BF16, false>(b);
-                out[3][p] = e4m3_16<BF16, true>(b);
+                out[0][p] = e4m3_16<false, false>(a);
+                out[1][p] = e4m3_16<false, true>(a);
+                out[2][p] = e4m3_16<false, false>(b);
+                out[3][p] = e4m3_16<false, true>(b);
             } else {
                 out[0][p] = bytes_of(y, x, 0x05040100);
                 out[1][p] = bytes_of(y, x, 0x07060302);
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
             }
         };
         auto take_unit = [&]() {
-            if constexpr (S::kUnit) {
+            if constexpr (E4M3) {
                 const float less = unit.take(v_scale);
                 if (less != 1.0f)
                     for (int t = 0; t < NT; ++t)
@@ -216,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     const f32x4 ks = *reinterpret_cast<const f32x4 *>(keys.k_scale[tile & 1] + 16 * i + 4 * g);
                     const f32x4 v = *reinterpret_cast<const f32x4 *>(keys.v_scale[tile & 1] + 16 * i + 4 * g);
                     for (int t = 0; t < NT; ++t) score[i][t] *= ks;
-                    for (int e = 0; e < 4; ++e) vs[4 * i + e] = S::kUnit ? v[e] * unit.inverse : v[e];
+                    for (int e = 0; e < 4; ++e) vs[4 * i + e] = E4M3 ? v[e] * unit.inverse : v[e];
                 } else {
                     for (int t = 0; t < NT; ++t) score[i][t] *= a.scale_log2;
                 }
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     sum[t] += e8[e];
                     if (E4M3) e8[e] *= vs[e];
                 }
-                for (int e = 0; e < 4; ++e) p[t][e] = BF16 ? pack_bf16(e8[2 * e], e8[2 * e + 1]) : pack_f16(e8[2 * e], e8[2 * e + 1]);
+                for (int e = 0; e < 4; ++e) p[t][e] = S::kPBf16 ? pack_bf16(e8[2 * e], e8[2 * e + 1]) : pack_f16(e8[2 * e], e8[2 * e + 1]);
             }
             constexpr int kAtOnce = E4M3 ? 4 : 2;        // dims from one word
             for (int w = 0; w < S::kVWords; ++w) {
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                 S::v_operands(x, w, v);
                 for (int e = 0; e < kAtOnce; ++e)
                     for (int t = 0; t < NT; ++t)
-                        acc[t][kAtOnce * w + e] = product16<BF16>(v[e], u32x4{p[t][0], p[t][1], p[t][2], p[t][3]}, acc[t][kAtOnce * w + e]);
+                        acc[t][kAtOnce * w + e] = product16<S::kPBf16>(v[e], u32x4{p[t][0], p[t][1], p[t][2], p[t][3]}, acc[t][kAtOnce * w + e]);
             }
             if (odd) {                                   // rare: such values reach the rows that see them, and no others
                 const int64_t seg = int64_t(D) * S::kElem;
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
             if (alone) {
                 const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div));
                 const int qh = h * a.group + row - token * a.group;
-                const float inv = sum[t] == 0 ? 0.0f : (S::kUnit ? unit.unit : 1.0f) / sum[t];
+                const float inv = sum[t] == 0 ? 0.0f : (E4M3 ? unit.unit : 1.0f) / sum[t];
                 uint8_t *o = a.out + (s.row0 + token) * a.out_stride + int64_t(qh) * (2 * D);
                 for (int e = 0; e < 4; ++e)
                     for (int d = 0; d < S::kDims; d += 2) {
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                 // Which of the two contexts that a range can share with others: the one that began before it, or the one that goes on.
                 float *o = a.partials + partial_at(a, worker, h, at != seq_begin ? 0 : 1, row, D);
                 for (int e = 0; e < 4; ++e)
-                    for (int d = 0; d < S::kDims; ++d) o[(4 * g + e) * S::kDims + d] = S::kUnit ? acc[t][d][e] * unit.unit : acc[t][d][e];
+                    for (int d = 0; d < S::kDims; ++d) o[(4 * g + e) * S::kDims + d] = E4M3 ? acc[t][d][e] * unit.unit : acc[t][d][e];
                 if (g == 0) o[D] = top[t], o[D + 1] = sum[t];
             }
         }
