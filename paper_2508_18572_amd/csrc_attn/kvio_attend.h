@@ -159,6 +159,28 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     }
 }
 
+// Whether any of some words has such an element.
+template <bool BF16, bool E4M3>
+struct NotFinite {
+    uint32_t most = 0;                       // of the elements' sizes, in each half; in e4m3 a byte's top bit for each
+    __device__ __forceinline__ void look(uint32_t w) {
+        if constexpr (E4M3) most |= (w & 0x7f7f7f7fu) + 0x01010101u;
+        else most = larger_halves(most, w & 0x7fff7fffu);
+    }
+    __device__ __forceinline__ bool found() const {
+        constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+        return E4M3 ? (most & 0x80808080u) != 0 : (most & 0xffffu) >= kExp || (most >> 16) >= kExp;
+    }
+};
+
+// The lowest n + 1 bits: none below 0, all from 31 on.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n < 0 ? 0u : n >= 31 ? ~0u : (2u << n) - 1u; }
+// v where bit n of `bits` is set, else w.
+__device__ __forceinline__ float where_bit(uint32_t bits, int n, float v, float w) {
+    const uint32_t m = static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - n)) >> 31);
+    return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) & m) | (__builtin_bit_cast(uint32_t, w) & ~m));
+}
+
 // Element i of a row of the cache.
 template <bool BF16, bool E4M3>
 __device__ __forceinline__ float element(const uint8_t *p, int i) {

@@ -145,7 +145,7 @@ struct Shape {
     static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 64;
     static constexpr bool kPBf16 = BF16 && !E4M3;        // probabilities' and values' type: fp16, in a ValueUnit, for e4m3 values
     // Operands in registers at a time; with fewer than a phase has, K of a tile is still read while the next but one is put.
-    static constexpr int kKOps = D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 3 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
+    static constexpr int kKOps = D == 128 && E4M3 ? 2 : D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 3 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
     struct alignas(16) Lds {
         uint8_t k[kKBuffers][kKeys * kKRow], v[2][kKeys * kVRow];
         float k_scale[4][64], v_scale[4][64];            // of tiles, by their number & 3
@@ -238,6 +238,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             return c.page_table[b * c.table_stride + static_cast<int>(div_by(static_cast<uint32_t>(key < c.max_ctx ? key : c.max_ctx - 1), c.page_div))];
         };
         float k_scale = 0, v_scale = 0;
+        f32x4 ks[2] = {}, vs[2] = {};                    // e4m3: scales of 4 g + 8 r .. + 3 of a half's keys, of r and r + 1; values' in value_unit
         ValueUnit value_unit;
         uint64_t there_now = 0;                          // the keys that are there
         int bad_page = -1;
@@ -259,17 +260,22 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             return there ? page * c.page_size + (key - i * c.page_size) : 0;
         };
         auto put_scales = [&](int tile, uint64_t there) KVIO_INLINE {
-            if constexpr (E4M3) {                    // long before the tile is worked on
-                const float less = value_unit.take((there >> lane) & 1 ? v_scale : 0.0f);
-                if (less != 1.0f)
+            if constexpr (!E4M3) return;
+            const bool is_there = (there >> lane) & 1;   // what garbage holds does not count
+            const float less = value_unit.take(is_there ? v_scale : 0.0f);
+            if (less != 1.0f) {                          // rare, and the same in all waves: what is in the old unit follows
 #pragma unroll
-                    for (int t = 0; t < kColumns; ++t)
+                for (int t = 0; t < kColumns; ++t)
 #pragma unroll
-                        for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
+                    for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
+                vs[0] *= less, vs[1] *= less;
+                workgroup_barrier();
+                if (wave < 4) lds.v_scale[wave][lane] *= less;
+                workgroup_barrier();
             }
-            if (E4M3 && wave == 0) {                     // what garbage holds does not count
-                lds.k_scale[tile & 3][lane] = (there >> lane) & 1 ? k_scale : 0.0f;
-                lds.v_scale[tile & 3][lane] = (there >> lane) & 1 ? v_scale : 0.0f;
+            if (wave == 0) {
+                lds.k_scale[tile & 3][lane] = is_there ? k_scale : 0.0f;
+                lds.v_scale[tile & 3][lane] = is_there ? v_scale * value_unit.inverse : 0.0f;
             }
         };
         const int piece = tid % S::kPieces, piece_row = tid / S::kPieces % kKeys;
@@ -307,19 +313,21 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         // Hidden values may hold anything: those that are not finite become zeros, the tile is marked.
         auto clean_v = [&](int tile, uint64_t there) KVIO_INLINE {
             if (whole_for_all(tile, there)) return;
-            bool odd = false;
+            if (there != ~0ull)
 #pragma unroll
-            for (int i = 0; i < S::kPasses; ++i) {
-                const bool is_there = (there >> (piece_row + i * S::kRowsAtOnce)) & 1;
+                for (int i = 0; i < S::kPasses; ++i)
+                    if (((there >> (piece_row + i * S::kRowsAtOnce)) & 1) == 0) vx[i] = u32x4{0, 0, 0, 0};
+            NotFinite<BF16, E4M3> any;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t v = is_there ? vx[i][e] : 0;
-                    const uint32_t bad = not_finite<BF16, E4M3>(v);
-                    odd = odd || bad != 0;
-                    vx[i][e] = v & ~bad;
-                }
-            }
-            if (odd) lds.odd[(serial + tile) & 3] = serial + tile;
+            for (int i = 0; i < S::kPasses; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any.look(vx[i][e]);
+            if (!wave_any(any.found())) return;
+#pragma unroll
+            for (int i = 0; i < S::kPasses; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vx[i][e] &= ~not_finite<BF16, E4M3>(vx[i][e]);
+            if (any.found()) lds.odd[(serial + tile) & 3] = serial + tile;
         };
 
         // ---- products, 32 keys at a time: half i of a tile ---------------------------------
@@ -327,7 +335,6 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         constexpr int kUnits = 8 * kColumns, kScoreProducts = S::kSteps * kColumns, kOutProducts = 2 * S::kDimBlocks * kColumns;
         f32x16 score[kColumns], ahead[kColumns];
         u32x4 k_op[S::kKOps], v_op[S::kVOps], p[kColumns][2];
-        f32x4 ks[2], vs[2];                              // e4m3: scales of 4 g + 8 r .. + 3 of a half's keys, of r and r + 1
         auto fetch_k = [&](int buffer, int i, int e) KVIO_INLINE {
             k_op[e % S::kKOps] = *reinterpret_cast<const u32x4 *>(lds.k[buffer] + (32 * i + m) * S::kKRow + 16 * g + 32 * e);
         };
@@ -364,23 +371,23 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             float y = exp2_fast(fmaf(x[t][e], unit, -from[t])), z = exp2_fast(fmaf(x[t][e + 1], unit, -from[t]));
             sum[t] += y + z;
             if (e == 14) keep_here(sum[t]);
-            if (E4M3) y *= value_unit.inverse, z *= value_unit.inverse;
             if (E4M3) y *= vs[e / 4 % 2][e % 4], z *= vs[e / 4 % 2][e % 4 + 1];
             p[t][e / 8][e / 2 % 4] = S::kPBf16 ? pack_bf16(y, z) : pack_f16(y, z);
         };
         auto mask = [&](int tile, int i, uint64_t there, f32x16 (&x)[kColumns]) KVIO_INLINE { // hidden keys at minus infinity
             const int base = base0 + tile * kKeys + 32 * i;
             if (idle || (base + 31 <= wave_first_place && (a.window == 0 || base > wave_last_place - a.window) && there == ~0ull)) return;
+            // Bit n of `seen`: the row sees key base + 4 g + n.
             const uint32_t mine = static_cast<uint32_t>(there >> (32 * i + 4 * g));
 #pragma unroll
-            for (int t = 0; t < kColumns; ++t) best[t] = kMinusInf;
+            for (int t = 0; t < kColumns; ++t) {
+                const int up_to = place[t] - (base + 4 * g);
+                uint32_t seen = mine & low_bits(up_to);
+                if (a.window > 0) seen &= ~low_bits(place[t] < 0 ? -1 : up_to - a.window);
+                best[t] = kMinusInf;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int at_key = 8 * (e / 4) + e % 4, key = base + at_key + 4 * g;
-                const bool is_there = (mine >> at_key) & 1;
-#pragma unroll
-                for (int t = 0; t < kColumns; ++t) {
-                    if (!(is_there && key <= place[t] && (a.window == 0 || key > place[t] - a.window))) x[t][e] = kMinusInf;
+                for (int e = 0; e < 16; ++e) {
+                    x[t][e] = where_bit(seen, 8 * (e / 4) + e % 4, x[t][e], kMinusInf);
                     best[t] = larger(best[t], x[t][e]);
                 }
             }

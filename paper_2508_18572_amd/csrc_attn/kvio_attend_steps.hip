@@ -154,6 +154,19 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
             for (int i = g; i < D / 8; i += 4)
                 *reinterpret_cast<u32x4 *>(keys.q[row] + 16 * i) = row < rows ? *reinterpret_cast<const u32x4 *>(p + 16 * i) : u32x4{0, 0, 0, 0};
         }
+        // A SIMD's only wave has the registers to keep Q's operands, and nobody to work while it waits for LDS.
+        constexpr bool kKeepQ = occupancy(E4M3, D, NT) == 1;
+        u32x4 q[kKeepQ ? NT : 1][kKeepQ ? S::kSteps : 1];
+        auto q_operand = [&](int t, int s2) __attribute__((always_inline)) {
+            return *reinterpret_cast<const u32x4 *>(keys.q[16 * t + m] + S::q_offset(s2, g));
+        };
+        if constexpr (kKeepQ) {
+            wave_lds_fence();
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int s2 = 0; s2 < S::kSteps; ++s2) q[t][s2] = q_operand(t, s2);
+        }
         f32x4 acc[NT][S::kDims];
         float top[NT], sum[NT];
         for (int t = 0; t < NT; ++t) {
@@ -208,9 +221,9 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                 for (int i = 0; i < 2; ++i) {
                     const u32x4 k = S::k_operand(x.k[i], s2);
                     for (int t = 0; t < NT; ++t)
-                        score[i][t] = product16<BF16>(k, *reinterpret_cast<const u32x4 *>(keys.q[16 * t + m] + S::q_offset(s2, g)), score[i][t]);
+                        score[i][t] = product16<BF16>(k, kKeepQ ? q[kKeepQ ? t : 0][kKeepQ ? s2 : 0] : q_operand(t, s2), score[i][t]);
                 }
-            if (tile + 1 < n) S::load_k(a, next_slot, h, lane, &x);
+            S::load_k(a, next_slot, h, lane, &x);        // also behind the last tile, of slot 0: loads on some paths only would be waited for on all
             float vs[8];
             for (int i = 0; i < 2; ++i) {
                 if (E4M3) {
@@ -292,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                         }
                 }
             }
-            if (tile + 1 < n) S::load_v(a, next_slot, h, lane, &x);
+            S::load_v(a, next_slot, h, lane, &x);
         };
 
         // A tile's pages are asked for two tiles ahead, and before the loads of the next tile, so that

@@ -47,6 +47,11 @@ __device__ __forceinline__ uint32_t e4m3_16(uint32_t w) {
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
 }
 
+// The larger of each half, as whole numbers.
+__device__ __forceinline__ uint32_t larger_halves(uint32_t a, uint32_t b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
 // Byte i of the result is byte (sel >> 8 i) & 7 of the eight in b (0 to 3) and a (4 to 7).
 __device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t sel) { return __builtin_amdgcn_perm(a, b, sel); }
 

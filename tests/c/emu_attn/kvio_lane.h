@@ -76,6 +76,10 @@ uint32_t e4m3_16(uint32_t w) {
     const f32x2 v = e4m3_f32<HIGH>(w);
     return BF16 ? pack_bf16(v.x, v.y) : pack_f16(v.x, v.y);
 }
+inline uint32_t larger_halves(uint32_t a, uint32_t b) {
+    const uint32_t l = (a & 0xffffu) > (b & 0xffffu) ? a & 0xffffu : b & 0xffffu, h = a >> 16 > b >> 16 ? a >> 16 : b >> 16;
+    return l | (h << 16);
+}
 inline uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t sel) {
     const uint64_t all = (uint64_t(a) << 32) | b;
     uint32_t r = 0;
