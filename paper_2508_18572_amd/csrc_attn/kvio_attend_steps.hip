@@ -37,7 +37,7 @@ struct alignas(16) WaveLds {
 
 // Waves to a SIMD for which the registers last without scratch.
 constexpr int occupancy(bool e4m3, int dim, int columns) {
-    return dim * columns <= 64 ? 4 : dim * columns <= 128 ? 3 : dim * columns <= 256 && (e4m3 || dim == 128) ? 2 : 1;
+    return dim * columns <= 64 ? 4 : dim * columns <= 128 ? 3 : dim * columns <= 256 && (dim == 64 ? columns < 4 : e4m3 || dim == 128) ? 2 : 1;
 }
 
 template <bool BF16, bool E4M3, int D, int NT>
@@ -50,6 +50,8 @@ struct Steps {
     // Probabilities take the cache's type; beside e4m3 values, whose scales they carry, fp16 (in bf16 their roundings were
     // the larger part of the result's error) in a ValueUnit.
     static constexpr bool kPBf16 = BF16 && !E4M3;
+    // An fp16 result shows that rounding too, where a context is short; there what it takes off is a second probability.
+    static constexpr bool kTwice = E4M3 && !BF16;
 
     struct Tile {
         uint32_t k[2][kKWords];
@@ -257,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     }
                 odd = wave_any(odd);
             }
-            uint32_t p[NT][4];
+            uint32_t p[NT][4], rest[S::kTwice ? NT : 1][4];
             for (int t = 0; t < NT; ++t) {
                 float best = score[0][t][0];
                 for (int i = 0; i < 2; ++i)
@@ -280,14 +282,19 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     if (E4M3) e8[e] *= vs[e];
                 }
                 for (int e = 0; e < 4; ++e) p[t][e] = S::kPBf16 ? pack_bf16(e8[2 * e], e8[2 * e + 1]) : pack_f16(e8[2 * e], e8[2 * e + 1]);
+                if constexpr (S::kTwice)
+                    for (int e = 0; e < 4; ++e) rest[t][e] = pack_f16(e8[2 * e] - f16_lo(p[t][e]), e8[2 * e + 1] - f16_hi(p[t][e]));
             }
             constexpr int kAtOnce = E4M3 ? 4 : 2;        // dims from one word
             for (int w = 0; w < S::kVWords; ++w) {
                 u32x4 v[kAtOnce];
                 S::v_operands(x, w, v);
                 for (int e = 0; e < kAtOnce; ++e)
-                    for (int t = 0; t < NT; ++t)
-                        acc[t][kAtOnce * w + e] = product16<S::kPBf16>(v[e], u32x4{p[t][0], p[t][1], p[t][2], p[t][3]}, acc[t][kAtOnce * w + e]);
+                    for (int t = 0; t < NT; ++t) {
+                        f32x4 &x4 = acc[t][kAtOnce * w + e];
+                        x4 = product16<S::kPBf16>(v[e], u32x4{p[t][0], p[t][1], p[t][2], p[t][3]}, x4);
+                        if constexpr (S::kTwice) x4 = product16<false>(v[e], u32x4{rest[t][0], rest[t][1], rest[t][2], rest[t][3]}, x4);
+                    }
             }
             if (odd) {                                   // rare: such values reach the rows that see them, and no others
                 const int64_t seg = int64_t(D) * S::kElem;
