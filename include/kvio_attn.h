@@ -98,7 +98,8 @@ kvio_status kvio_append(kvio_pool_t pool, int32_t layer, const kvio_append_args 
  * g = h / (num_q_heads / H), t over the context tokens up to the row's own and, with
  * window > 0, the last `window` of those only.  A row that sees no token gets zeros and an lse
  * of minus infinity; lse[row][h] (if not NULL) is the natural logarithm of the softmax's sum.
- * What hidden tokens hold, infinities and NaN included, has no effect.
+ * What hidden tokens hold, infinities and NaN included, has no effect, nor have scales, such ones included, of pages that
+ * a row sees no token of (but for the precision that is named below).
  * Products are accumulated in fp32, probabilities rounded to the cache's type for the second one; with an
  * e4m3 cache to fp16, times their values' scales (a scale below 2^-18 of the context's largest loses precision).
  * Equal inputs give equal bits, except over other max_pages, max_query or GPUs.

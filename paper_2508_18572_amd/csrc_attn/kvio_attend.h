@@ -128,24 +128,37 @@ __device__ __forceinline__ void rows_without_keys(const AttendArgs &a, int h, in
     }
 }
 
+__device__ __forceinline__ bool is_finite(float v) { return v - v == 0; }
+
 // fp16 probabilities meet e4m3 values with these' scales, in units of a power of two that follows the largest scale so far:
 // products with probabilities (up to 2^8) stay below 2^15, and far smaller scales keep their precision.  Of a wave; out^T is
 // kept in that unit.
 struct ValueUnit {
     float unit = 0x1p-120f, inverse = 0x1p120f;
-    // `scale`: of the lane's key (0 for none).  What out^T has to be multiplied by.
-    __device__ __forceinline__ float take(float scale) {
+    // `scale`: of the lane's key (0 for none).  What out^T has to be multiplied by.  A scale that is infinite or NaN becomes 0
+    // (a hidden key's probability, 0, times it would be NaN) and sets `odd`: such keys' values are added on their own.
+    __device__ __forceinline__ float take(float &scale, bool &odd) {
         const float size = fabsf(scale);
-        if (!wave_any(size > 128 * unit)) return 1.0f;
-        float most = size <= 0x1p120f ? size : 0.0f;
+        odd = false;
+        if (!wave_any(!(size * 0x1p-7f <= unit))) return 1.0f;
+        const bool finite = is_finite(scale);
+        odd = wave_any(!finite);
+        if (!finite) scale = 0;
+        float most = fabsf(scale);
         for (int by = 1; by < 64; by *= 2) most = fmaxf(most, lane_xor(most, by));
-        if (!(most > 128 * unit)) return 1.0f;
+        if (most * 0x1p-7f <= unit) return 1.0f;
         const float before = unit;
         unit = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, most) & 0x7f800000u)) * 0x1p-6f;
         inverse = 1.0f / unit;
         return before * inverse;
     }
 };
+
+// What a code of an odd value is multiplied by to give an infinity or NaN, or to stay what it is.
+__device__ __forceinline__ float odd_scale_at(const AttendArgs &a, int page, int h) {
+    const float s = a.c.v_scale[page * a.c.scale_stride + h];
+    return is_finite(s) ? 1.0f : s;
+}
 
 // Ones where an element of the word, two of 16 bits or four codes, is infinite or NaN.
 template <bool BF16, bool E4M3>
@@ -181,7 +194,7 @@ __device__ __forceinline__ float where_bit(uint32_t bits, int n, float v, float 
     return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) & m) | (__builtin_bit_cast(uint32_t, w) & ~m));
 }
 
-// Element i of a row of the cache.
+// Element i of a row of the cache, as coded.
 template <bool BF16, bool E4M3>
 __device__ __forceinline__ float element(const uint8_t *p, int i) {
     if constexpr (E4M3) return e4m3_f32<false>(p[i]).x;

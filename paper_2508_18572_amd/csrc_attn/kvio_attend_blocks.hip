@@ -149,7 +149,7 @@ struct Shape {
     struct alignas(16) Lds {
         uint8_t k[kKBuffers][kKeys * kKRow], v[2][kKeys * kVRow];
         float k_scale[4][64], v_scale[4][64];            // of tiles, by their number & 3
-        int32_t odd[4];                                  // the running number of a tile with values that are not finite
+        int32_t odd[4];                                  // the running number of a tile with values that are not finite, or that has such scales
     };
 };
 
@@ -262,7 +262,9 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         auto put_scales = [&](int tile, uint64_t there) KVIO_INLINE {
             if constexpr (!E4M3) return;
             const bool is_there = (there >> lane) & 1;   // what garbage holds does not count
-            const float less = value_unit.take(is_there ? v_scale : 0.0f);
+            float vs_now = is_there ? v_scale : 0.0f;
+            bool odd;
+            const float less = value_unit.take(vs_now, odd);
             if (less != 1.0f) {                          // rare, and the same in all waves: what is in the old unit follows
 #pragma unroll
                 for (int t = 0; t < kColumns; ++t)
@@ -275,7 +277,8 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             }
             if (wave == 0) {
                 lds.k_scale[tile & 3][lane] = is_there ? k_scale : 0.0f;
-                lds.v_scale[tile & 3][lane] = is_there ? v_scale * value_unit.inverse : 0.0f;
+                lds.v_scale[tile & 3][lane] = vs_now * value_unit.inverse;
+                if (odd) lds.odd[(serial + tile) & 3] = serial + tile;
             }
         };
         const int piece = tid % S::kPieces, piece_row = tid / S::kPieces % kKeys;
@@ -418,11 +421,12 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                 if (page < 0) continue;
                 const int j = static_cast<int>(div_by(static_cast<uint32_t>(key), c.page_div));
                 const uint8_t *v = c.v_cache + (int64_t(page) * c.page_size + (key - j * c.page_size)) * cache_row + h * S::kSeg;
+                const float by = E4M3 ? odd_scale_at(a, page, h) : 1.0f;
 #pragma unroll
                 for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float f = element<BF16, E4M3>(v, 32 * d + 8 * (e / 4) + 4 * g + e % 4);
+                        const float f = element<BF16, E4M3>(v, 32 * d + 8 * (e / 4) + 4 * g + e % 4) * by;
                         in_order();
                         if (!wave_any(f - f != 0)) continue;
 #pragma unroll

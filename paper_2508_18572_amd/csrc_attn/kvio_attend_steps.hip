@@ -196,9 +196,10 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                 v_scale = there ? c.v_scale[page * c.scale_stride + h] : 0.0f;
             }
         };
+        bool odd_scale = false;                          // in the tile whose scales were put last
         auto take_unit = [&]() {
             if constexpr (E4M3) {
-                const float less = unit.take(v_scale);
+                const float less = unit.take(v_scale, odd_scale);
                 if (less != 1.0f)
                     for (int t = 0; t < NT; ++t)
                         for (int d = 0; d < S::kDims; ++d) acc[t][d] *= less;
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
             }
             // Keys that some row does not see, or that are not there, are masked; their values may hold anything.
             const bool whole = base >= span.whole_lo && base + kTile <= span.whole_hi;
-            bool odd = false;                            // a value that is not finite where it matters
+            bool odd = odd_scale;                        // a value that is not finite where it matters
             if (!whole || wave_any(slot[lane & 31] < 0)) {
                 for (int i = 0; i < 2; ++i)
                     for (int e = 0; e < 4; ++e) {
@@ -302,9 +303,10 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     const int one = slot[at_key], key = base + at_key;
                     if (one < 0) continue;
                     const uint8_t *v = c.v_cache + one * (seg * c.heads) + h * seg;
+                    const float by = E4M3 ? odd_scale_at(a, static_cast<int>(div_by(static_cast<uint32_t>(one), c.page_div)), h) : 1.0f;
                     for (int e = 0; e < 4; ++e)
                         for (int d = 0; d < S::kDims; ++d) {
-                            const float f = element<BF16, E4M3>(v, (4 * g + e) * S::kDims + d);
+                            const float f = element<BF16, E4M3>(v, (4 * g + e) * S::kDims + d) * by;
                             in_order();                  // one at a time: registers matter here, time does not
                             if (!wave_any(f - f != 0)) continue;
                             for (int t = 0; t < NT; ++t)

@@ -1,0 +1,30 @@
+"""append and attend on an MI355X at the ends of what their arguments may hold."""
+import math
+
+import pytest
+
+from test_gpu_attn import filled, kv, on_gpu  # noqa: F401  (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("odd", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("D,new", [(64, 4), (64, 90), (128, 5), (128, 12), (128, 100), (256, 3), (256, 70)])
+def test_a_hidden_tokens_scale_has_no_effect(kv, D, new, dtype, odd):  # noqa: F811
+    """The last token's page, of one token, gets such a scale of values: the rows before it stay as they are."""
+    import torch
+    c = filled(8, getattr(torch, dtype), 8, 2, D, 1, [(700, new), (40, 3)], seed=new)
+    g, pool, batch = on_gpu(kv, c)
+    lses = [torch.empty(g["q"].shape[:2], device="cuda") for _ in range(2)]
+    clean = pool.attend(0, batch, g["q"], lse=lses[0])
+    page = int(c["table"][0, 700 + new - 1])
+    g["scales"][1, 0, page, 0] = odd
+    got = pool.attend(0, batch, g["q"], lse=lses[1])
+    assert torch.equal(got[:new - 1], clean[:new - 1]) and torch.equal(got[new:], clean[new:]) and torch.equal(*lses)
+    assert torch.equal(got[new - 1, 4:], clean[new - 1, 4:])
+    code = g["pool"].view(torch.float8_e4m3fn)[1, 0, page, 0].float()
+    want = (code * odd).to(got.dtype)                              # nothing finite counts beside it
+    row = got[new - 1, :4]
+    assert bool(((row == want) | (row.isnan() & want.isnan())).all())
+    pool.close()
