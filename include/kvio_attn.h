@@ -65,9 +65,9 @@ typedef struct kvio_batch {
  * In e4m3 a page's scale of a head is the smallest power of two 2^e, e >= -100,
  * with all elements that the page has taken since its first token within 448 * 2^e: a page whose
  * first token is among the new ones starts anew, one that is filled further
- * keeps its scale unless new elements pass 448 times it; then its rows are
- * rounded again under the new one (exact but for codes below the smallest
- * normal one, as scales are powers of two).  Elements are rounded to nearest even; infinities
+ * keeps its scale unless new elements pass 448 times it, or it is (from elsewhere) below 2^-100 in size,
+ * infinite or NaN; then its rows are rounded again under the new one (exact but for codes below the smallest
+ * normal one, where both are powers of two).  Elements are rounded to nearest even; infinities
  * become +-448 times the scale and do not raise it, NaN stays NaN.
  * No two rows of a call may name one pool slot, in e4m3 no two sequences one page
  * that they append to.  Rows of no sequence are left alone, in q_out too. */

@@ -132,7 +132,9 @@ __device__ __forceinline__ float scale_for(float top) {
 // v * inv as an e4m3 value: within +-448, NaN kept.
 __device__ __forceinline__ float within(float v) { return v != v ? v : fminf(fmaxf(v, -448.0f), 448.0f); }
 
-__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) <= 3.4e38f ? fabsf(v) : 0.0f; }
+constexpr float kLargest = 3.402823466e38f;
+
+__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) <= kLargest ? fabsf(v) : 0.0f; }
 
 template <bool BF16>
 __device__ __forceinline__ u32x2 codes_of(u32x4 x, float inv) {
@@ -233,10 +235,12 @@ __device__ __forceinline__ void append_page(const AppendArgs &a, int group, f32x
     for (int by = 1; by < 64; by *= 2) top = fmaxf(top, lane_xor(top, by));
     float scale = scale_for(top);
     if (from != begin) {
-        if (top <= 448.0f * was) {
+        // Not one that nothing can be divided by (a page of zeros from elsewhere may have 0).
+        const float size = fabsf(was);
+        if (size >= 0x1p-100f && size <= kLargest && top <= 448.0f * size) {
             scale = was;
         } else {
-            const float by = was / scale;    // below one
+            const float by = was / scale;    // below one in size, or infinite or NaN
             for (int t = sub; t < from - begin; t += per_pass) {
                 if (!mine) continue;
                 u32x4 *row = reinterpret_cast<u32x4 *>(cache + t * cache_row + 16 * j);

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import test_emulated_kernels as base
-from _attn_plain import append_plain, values
+from _attn_plain import values
 from test_attn_blocks_emulated import attend, case
 from test_attn_emulated import TYPE, Box, batch_args, emu, make_pool  # noqa: F401  (a fixture)
 
@@ -43,3 +43,46 @@ def test_scales_that_all_rows_see(emu, new, dtype, odd):  # noqa: F811
     out, _ = attend(emu, c)
     out = out[:new]
     assert bool(out.isnan().all()) if math.isnan(odd) else bool((out[..., ::2] == -math.inf).any() and (out[..., 1::2] == math.inf).any())
+
+
+BEGUN = [(0.0, 0.0), (0.0, 1.5), (-0.0, 0.0), (2.0 ** -140, 0.0), (2.0 ** -128, 0.0), (2.0 ** -127, 2.0 ** -130), (2.0 ** -101, 0.0), (2.0 ** -100, 0.0),
+         (2.0 ** -99, 2.0 ** -92), (0.75, 300.0), (0.75, 340.0), (-0.5, 100.0), (-0.5, 300.0), (2.0 ** 127, 1.0), (math.inf, 1.0), (math.inf, 0.0),
+         (math.nan, 2.0), (math.nan, 0.0)]
+
+
+@pytest.mark.parametrize("was,top", BEGUN)
+@pytest.mark.parametrize("new", [1, 9])
+def test_append_to_a_begun_page_of_any_scale(emu, new, was, top):  # noqa: F811
+    """A page whose scale came from elsewhere keeps it where it is a number of at least 2^-100 in size whose 448-fold holds the new
+    rows; else the rows that are there are rounded again under the new one."""
+    kv, lib, A = emu
+    H, D, P, had = 2, 64, 16, 5
+    gen = torch.Generator().manual_seed(new)
+    codes = torch.randint(0, 256, (2, P, H, D), generator=gen).to(torch.uint8)
+    box = Box(kv)
+    pool, h = make_pool(kv, box, {"H": H, "D": D, "P": P, "pool": codes.view(torch.float8_e4m3fn)})
+    rows = torch.rand(2, new, H, D, generator=gen) * 2 - 1
+    rows[:, -1, :, 7] = -1
+    rows = (rows * top).bfloat16()
+    a = A.kvio_append_args(batch=batch_args(A, box, None, torch.zeros(1, 1, dtype=torch.int32), torch.tensor([had + new], dtype=torch.int32),
+                                            torch.tensor([0, new], dtype=torch.int32), new), dtype=0, cache_dtype=2)
+    (_, a.k), (_, a.v) = box.put(rows[0]), box.put(rows[1])
+    a.k_stride = a.v_stride = H * D
+    scales, a.k_scale = box.put(torch.full((2, 1, H), was))
+    a.v_scale, a.scale_stride = a.k_scale + 4 * H, H
+    assert lib.kvio_append(h, 0, ctypes.byref(a), None) == 0, kv.kvio_last_error()
+    top = float(rows.double().abs().max())
+    need = 2.0 ** max(-100, math.ceil(math.log2(top / 448))) if top else 2.0 ** -100
+    now = was if 2.0 ** -100 <= abs(was) < math.inf and top <= 448 * abs(was) else need
+    assert bool((scales == now).all()), (scales, now)
+    want = torch.cat((values(codes[:, :had]) * was, rows.double()), 1) / now
+    want = torch.where(want.isnan(), want, want.clamp(-448, 448))
+    got = values(pool)[:, :had + new]
+    assert torch.equal(got.isnan(), want.isnan())
+    # half a step of e4m3: 2^-4 relative, 2^-10 below its normal range; a quotient in 32 bits is off by 2^-23 of itself
+    ok = (got - want).abs() <= want.abs().clamp(min=2.0 ** -6) * 2.0 ** -4 * (1 + 2.0 ** -19)
+    assert bool((ok | want.isnan()).all())
+    assert now != was or torch.equal(pool.view(torch.uint8)[:, :had], codes[:, :had])
+    assert torch.equal(pool.view(torch.uint8)[:, had + new:], codes[:, had + new:])
+    kv.kvio_pool_destroy(h)
+    box.free()

@@ -28,3 +28,28 @@ def test_a_hidden_tokens_scale_has_no_effect(kv, D, new, dtype, odd):  # noqa: F
     row = got[new - 1, :4]
     assert bool(((row == want) | (row.isnan() & want.isnan())).all())
     pool.close()
+
+
+@pytest.mark.parametrize("was,now", [(0.0, 2.0 ** -100), (2.0 ** -140, 2.0 ** -100), (2.0 ** -101, 2.0 ** -100), (math.inf, 2.0 ** -100),
+                                     (2.0 ** -100, 2.0 ** -100), (0.75, 0.75)])
+def test_append_zeros_to_a_begun_page_of_any_scale(kv, was, now):  # noqa: F811
+    """Rows of zeros stay zeros, and a scale that codes cannot be divided by is replaced."""
+    import torch
+    H, D, P = 4, 128, 16
+    codes = torch.full((2, 1, 2 * P, H, D), 0x38, dtype=torch.uint8, device="cuda")                # 1.0
+    scales = torch.full((2, 1, 2, H), was, device="cuda")
+    pool = kv.KVPool(codes, P, scales=scales)
+    batch = kv.Batch(torch.tensor([[1, 0]], dtype=torch.int32, device="cuda"), torch.tensor([7], dtype=torch.int32, device="cuda"))
+    zeros = torch.zeros(1, H, D, dtype=torch.bfloat16, device="cuda")
+    pool.append(0, batch, zeros, zeros)
+    assert bool((scales[:, 0, 1] == now).all()) and bool((scales[:, 0, 0] == was).all())
+    assert bool((codes[:, 0, P + 6] == 0).all())                   # the seventh token
+    old = {True: 0x38}.get(was == now, 0x7e if was == math.inf else None)
+    rest = codes[:, 0, P:P + 6]
+    if old is not None:
+        assert bool((rest == old).all())
+    else:                                                          # 1.0 times `was`, under 2^-100
+        want = torch.tensor(was / now).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        assert bool((rest == want).all())
+    assert bool((codes[:, 0, :P] == 0x38).all()) and bool((codes[:, 0, P + 7:] == 0x38).all())
+    pool.close()
