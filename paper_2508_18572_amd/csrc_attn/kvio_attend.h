@@ -16,12 +16,17 @@ struct Span {
     int32_t lo, hi, whole_lo, whole_hi;
     int32_t tiles;                           // of kTile keys, at multiples of it, that hold [lo, hi)
 };
+// The first key that a row at `place` sees; both may be so far from 0 that 32 bits do not hold their difference.
+__device__ __forceinline__ int32_t window_from(const AttendArgs &a, int place) {
+    const int64_t from = int64_t(place) - a.window + 1;
+    return a.window > 0 && from > 0 ? static_cast<int32_t>(from) : 0;
+}
 __device__ __forceinline__ Span span_of(const AttendArgs &a, const Seq &s) {
     Span r;
     const int last = s.first + s.rows - 1;   // the last row's place
     r.hi = last + 1;
-    r.lo = a.window > 0 && s.first - a.window + 1 > 0 ? s.first - a.window + 1 : 0;
-    r.whole_lo = a.window > 0 && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
+    r.lo = window_from(a, s.first);
+    r.whole_lo = window_from(a, last);
     r.whole_hi = s.first + 1;
     r.tiles = s.rows > 0 && r.hi > r.lo ? (r.hi + kTile - 1) / kTile - r.lo / kTile : 0;
     return r;

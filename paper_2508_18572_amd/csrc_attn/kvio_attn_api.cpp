@@ -246,7 +246,7 @@ kvio_status kvio_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *ar
     a.out_stride = args->out_stride * 2;
     a.q_heads = args->num_q_heads;
     a.group = args->num_q_heads / p->g.num_heads;
-    a.window = args->window;
+    a.window = args->window < a.c.max_ctx ? args->window : 0;      // a longer one hides nothing
     a.scale_log2 = args->softmax_scale * 1.44269504088896340736f;
     a.group_div = kvio::divider(a.group);
     const kvio::AttendPlan plan = plan_of(p, *args);

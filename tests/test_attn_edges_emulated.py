@@ -86,3 +86,21 @@ def test_append_to_a_begun_page_of_any_scale(emu, new, was, top):  # noqa: F811
     assert torch.equal(pool.view(torch.uint8)[:, had + new:], codes[:, had + new:])
     kv.kvio_pool_destroy(h)
     box.free()
+
+
+LONGEST = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("window", [LONGEST, LONGEST - 40, 91, 90])
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("G", [1, 8])
+def test_windows_longer_than_the_context(emu, G, bits, window):  # noqa: F811
+    """More new tokens than the context has, 64 or fewer rows to a KV head and more: as without a window, bit for bit."""
+    c = case(torch.bfloat16, bits, 1, G, 64, 16, [(0, 60), (30, 20), (0, 5)], seed=12)
+    c["ctx"][0], c["ctx"][2] = 30, 1
+    c["max_query"] = 60
+    out, lse = attend(emu, c)
+    assert bool((out[30:60] != 0).any(2).all()) and bool((out[84] != 0).any())
+    c["window"] = window
+    got, got_lse = attend(emu, c)
+    assert torch.equal(got, out) and torch.equal(got_lse, lse)

@@ -53,3 +53,19 @@ def test_append_zeros_to_a_begun_page_of_any_scale(kv, was, now):  # noqa: F811
         assert bool((rest == want).all())
     assert bool((codes[:, 0, :P] == 0x38).all()) and bool((codes[:, 0, P + 7:] == 0x38).all())
     pool.close()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("D,new", [(64, 16), (128, 7), (128, 90), (256, 70)])
+def test_windows_longer_than_the_context(kv, D, new, bits):  # noqa: F811
+    """A window that hides nothing gives the bits of none, also where contexts have fewer tokens than are new."""
+    import torch
+    c = filled(bits, torch.bfloat16, 8, 2, D, 16, [(300, new), (0, new), (0, new)], seed=D + new)
+    c["ctx"][1] = new // 2
+    g, pool, batch = on_gpu(kv, c)
+    want = pool.attend(0, batch, g["q"])
+    row = new + new - new // 2
+    assert bool((want[new:row] == 0).all()) and bool((want[row:] != 0).any(2).all())
+    for window in (300 + new, 2 ** 31 - 1):
+        assert torch.equal(want, pool.attend(0, batch, g["q"], window=window))
+    pool.close()
