@@ -110,7 +110,7 @@ typedef struct kvio_attend_args {
     int32_t cache_dtype;        /* of the pool: `dtype` itself or KVIO_E4M3                  */
     int32_t num_q_heads;        /* a multiple of the pool's H                                */
     int32_t window;             /* 0 = none                                                  */
-    float softmax_scale;        /* > 0                                                       */
+    float softmax_scale;        /* > 0, and finite times log2(e)                             */
     int32_t reserved;           /* 0                                                         */
     const void *q;              /* [N][num_q_heads][D], tokens q_stride elements apart       */
     void *out;                  /* [N][num_q_heads][D], out_stride apart                     */

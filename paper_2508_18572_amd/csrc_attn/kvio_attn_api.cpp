@@ -121,6 +121,8 @@ kvio_status check_cache(kvio_pool_t p, int32_t layer, const kvio_batch &b, bool 
     return KVIO_OK;
 }
 
+constexpr float kLog2E = 1.44269504088896340736f;
+
 // Rows of a KV head that kvio_attend_steps.hip holds in a wave's registers, by the size of heads.
 int64_t most_step_rows(int64_t dim) { return dim <= 128 ? 64 : 32; }
 
@@ -136,7 +138,8 @@ kvio_status check_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *a
     if (group > kvio::block_rows(static_cast<int>(dim)))
         return fail(KVIO_EINVAL, "%s: %d query heads to a KV head; up to %d are built", fn, group, kvio::block_rows(static_cast<int>(dim)));
     if (args->window < 0) return fail(KVIO_EINVAL, "%s: window %d < 0", fn, args->window);
-    if (!(args->softmax_scale > 0) || !isfinite(args->softmax_scale)) return fail(KVIO_EINVAL, "%s: softmax_scale must be positive and finite", fn);
+    if (!(args->softmax_scale > 0) || !isfinite(args->softmax_scale * kLog2E))
+        return fail(KVIO_EINVAL, "%s: softmax_scale must be positive, and finite times log2(e)", fn);
     if (args->reserved != 0) return fail(KVIO_EINVAL, "%s: reserved is not 0", fn);
     const int64_t tiles = (int64_t(args->batch.max_pages) * p->g.page_size + 63) / 32;
     if (args->batch.num_seqs > 0 && args->batch.num_tokens > 0 && tiles * args->batch.num_seqs > INT32_MAX - 4096)
@@ -247,7 +250,7 @@ kvio_status kvio_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *ar
     a.q_heads = args->num_q_heads;
     a.group = args->num_q_heads / p->g.num_heads;
     a.window = args->window < a.c.max_ctx ? args->window : 0;      // a longer one hides nothing
-    a.scale_log2 = args->softmax_scale * 1.44269504088896340736f;
+    a.scale_log2 = args->softmax_scale * kLog2E;
     a.group_div = kvio::divider(a.group);
     const kvio::AttendPlan plan = plan_of(p, *args);
     a.partials = static_cast<float *>(args->workspace);

@@ -104,3 +104,35 @@ def test_windows_longer_than_the_context(emu, G, bits, window):  # noqa: F811
     c["window"] = window
     got, got_lse = attend(emu, c)
     assert torch.equal(got, out) and torch.equal(got_lse, lse)
+
+
+def small_attend(kv, lib, A, width=4 * 64, rows=6):
+    """One context of 40 tokens, 5 of them new, over a 16-bit pool; q and out in one buffer of `width` elements a row."""
+    box, H, Hq, D, P, pages, N = Box(kv), 2, 4, 64, 16, 3, 5
+    gen = torch.Generator().manual_seed(3)
+    codes = torch.randn(2, pages * P, H, D, generator=gen).bfloat16()
+    _, h = make_pool(kv, box, {"H": H, "D": D, "P": P, "pool": codes})
+    a = A.kvio_attend_args(batch=batch_args(A, box, None, torch.tensor([[0, 1, 2]], dtype=torch.int32), torch.tensor([40], dtype=torch.int32),
+                                            torch.tensor([0, N], dtype=torch.int32), N), num_q_heads=Hq, softmax_scale=0.125)
+    fused, at = box.put(torch.randn(rows, width, generator=gen).bfloat16())
+    a.q, a.out, a.q_stride, a.out_stride = at, at, width, width
+    need = ctypes.c_size_t()
+    assert lib.kvio_attend_workspace(h, ctypes.byref(a), ctypes.byref(need)) == 0
+    a.workspace, a.workspace_bytes = box.put(torch.zeros(max(need.value, 16), dtype=torch.uint8))[1], need.value
+    return a, h, box, fused
+
+
+@pytest.mark.parametrize("scale,fits", [(2.3e38, True), (2.4e38, False), (3.4e38, False), (1e-45, True), (-1.0, False), (math.nan, False)])
+def test_softmax_scales(emu, scale, fits):  # noqa: F811
+    """Scores are kept in powers of two: the scale times log2(e) has to be finite too (it would make NaN of a score of 0)."""
+    kv, lib, A = emu
+    a, h, box, _ = small_attend(kv, lib, A, width=8 * 64)
+    a.out = a.q + 2 * 4 * 64 * 6
+    a.q_stride = a.out_stride = 4 * 64
+    a.softmax_scale = scale
+    assert lib.kvio_attend(h, 0, ctypes.byref(a), None) == (0 if fits else kv.KVIO_EINVAL), kv.kvio_last_error()
+    assert fits or "softmax_scale" in kv.kvio_last_error()
+    need = ctypes.c_size_t()
+    assert lib.kvio_attend_workspace(h, ctypes.byref(a), ctypes.byref(need)) == (0 if fits else kv.KVIO_EINVAL)
+    kv.kvio_pool_destroy(h)
+    box.free()
