@@ -82,7 +82,8 @@ typedef struct kvio_append_args {
     int32_t reserved;           /* 0                                                         */
     const void *k, *v;          /* [N][H][D], tokens k_stride / v_stride elements apart      */
     const void *q;              /* [N][num_q_heads][D] or NULL                               */
-    void *q_out;                /* where rotated q goes: q itself, or memory apart from it   */
+    void *q_out;                /* where rotated q goes: q itself, or memory apart from it (slices of one */
+                                /*   buffer's rows are, where the strides are equal)         */
     int64_t k_stride, v_stride, q_stride, q_out_stride;  /* multiples of 8                   */
     const float *inv_freq;      /* fp32[rot_dim / 2]                                         */
     const int32_t *positions;   /* int32[N] or NULL                                          */
@@ -122,7 +123,7 @@ typedef struct kvio_attend_args {
     size_t workspace_bytes;     /*   need not survive between calls, overlapping calls need their own */
 } kvio_attend_args;
 
-/* D of 64, 128 or 256; q and out 16-byte aligned, memory apart from each other. */
+/* D of 64, 128 or 256; q and out 16-byte aligned, memory apart from each other (as q and q_out above). */
 kvio_status kvio_attend(kvio_pool_t pool, int32_t layer, const kvio_attend_args *args, hipStream_t stream);
 
 /* Bytes of workspace that kvio_attend takes for these arguments; follows from the batch's sizes and

@@ -39,10 +39,14 @@ kvio_status check_rows(kvio_pool_t p, const void *ptr, int64_t n, int64_t stride
     return check_array(p, ptr, reach(n, stride, heads * dim * 2), 16, fn, what);
 }
 
-// Whether `out` overlaps an input in another way than being it, row for row.
-bool overlaps(const void *a, uint64_t an, const void *b, uint64_t bn) {
+// Whether two arrays of n rows of `row` bytes, `a_stride` and `b_stride` elements apart, may share memory.  Rows equally far
+// apart (slices of one buffer) are looked at one by one, others as the whole ranges that they lie in.
+bool overlaps(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int64_t n, int64_t row) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return an != 0 && bn != 0 && x < y + bn && y < x + an;
+    if (n == 0 || x >= y + reach(n, b_stride, row) || y >= x + reach(n, a_stride, row)) return false;
+    if (n == 1 || a_stride != b_stride) return true;
+    const uint64_t step = uint64_t(a_stride) * 2, off = (x > y ? x - y : y - x) % step;
+    return off < uint64_t(row) || step - off < uint64_t(row);
 }
 
 kvio_status check_device(kvio_pool_t p, const char *fn) {
@@ -192,7 +196,7 @@ kvio_status kvio_append(kvio_pool_t p, int32_t layer, const kvio_append_args *ar
     if (st == KVIO_OK && args->positions != nullptr) st = check_array(p, args->positions, uint64_t(N) * 4, 4, fn, "positions");
     if (st != KVIO_OK) return st;
     if (with_q && !(args->q_out == args->q && args->q_out_stride == args->q_stride) &&
-        overlaps(args->q_out, reach(N, args->q_out_stride, args->num_q_heads * D * 2), args->q, reach(N, args->q_stride, args->num_q_heads * D * 2)))
+        overlaps(args->q_out, args->q_out_stride, args->q, args->q_stride, N, args->num_q_heads * D * 2))
         return fail(KVIO_EINVAL, "%s: q_out overlaps q without being it", fn);
     a.k = static_cast<const uint8_t *>(args->k);
     a.v = static_cast<const uint8_t *>(args->v);
@@ -240,7 +244,7 @@ kvio_status kvio_attend(kvio_pool_t p, int32_t layer, const kvio_attend_args *ar
     if (st == KVIO_OK) st = check_rows(p, args->out, N, args->out_stride, Hq, D, fn, "out");
     if (st == KVIO_OK && args->lse != nullptr) st = check_array(p, args->lse, uint64_t(N) * uint64_t(Hq) * 4, 4, fn, "lse");
     if (st != KVIO_OK) return st;
-    if (overlaps(args->out, reach(N, args->out_stride, Hq * D * 2), args->q, reach(N, args->q_stride, Hq * D * 2)))
+    if (overlaps(args->out, args->out_stride, args->q, args->q_stride, N, Hq * D * 2))
         return fail(KVIO_EINVAL, "%s: out overlaps q", fn);
     a.q = static_cast<const uint8_t *>(args->q);
     a.out = static_cast<uint8_t *>(args->out);

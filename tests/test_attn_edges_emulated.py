@@ -136,3 +136,34 @@ def test_softmax_scales(emu, scale, fits):  # noqa: F811
     assert lib.kvio_attend_workspace(h, ctypes.byref(a), ctypes.byref(need)) == (0 if fits else kv.KVIO_EINVAL)
     kv.kvio_pool_destroy(h)
     box.free()
+
+
+@pytest.mark.parametrize("q_at,out_at,fits", [(0, 256, True), (256, 0, True), (0, 512, True), (512, 0, True), (128, 400, True), (0, 248, False), (256, 8, False),
+                                              (0, 768 + 8, False), (0, 768 + 256, True), (768 + 512, 248, True), (520, 768, False), (512, 768, True), (0, 0, False)])
+def test_slices_of_one_buffer(emu, q_at, out_at, fits):  # noqa: F811
+    """q and out as slices of rows of 768 elements, 256 each: apart from each other in every row, or refused."""
+    kv, lib, A = emu
+    a, h, box, fused = small_attend(kv, lib, A, width=768, rows=7)
+    clean = fused.clone()
+    at = a.q
+    a.q, a.out = at + 2 * q_at, at + 2 * out_at
+    assert lib.kvio_attend(h, 0, ctypes.byref(a), None) == (0 if fits else kv.KVIO_EINVAL), kv.kvio_last_error()
+    assert fits or "overlaps" in kv.kvio_last_error()
+    got, flat = fused.view(-1)[out_at:][:4 * 768 + 256].clone(), clean.view(-1)
+    for i in range(5):                               # the same from a buffer of its own; nothing else is written
+        assert torch.equal(fused.view(-1)[q_at + i * 768:][:256], flat[q_at + i * 768:][:256])
+    if fits:
+        fused.copy_(clean)
+        a.out, a.out_stride = box.put(torch.zeros(5, 256, dtype=torch.bfloat16))[1], 256
+        own = torch.from_numpy(box.all[-1].array).view(torch.bfloat16).view(5, 256)
+        assert lib.kvio_attend(h, 0, ctypes.byref(a), None) == 0
+        for i in range(5):
+            assert torch.equal(got[i * 768:][:256], own[i])
+    # of append, the same check
+    b = A.kvio_append_args(batch=a.batch, num_q_heads=4, q=at + 2 * q_at, q_out=at + 2 * out_at, q_stride=768, q_out_stride=768, k_stride=128, v_stride=128)
+    b.k, b.v = (box.put(torch.zeros(5, 2, 64, dtype=torch.bfloat16))[1] for _ in range(2))
+    assert lib.kvio_append(h, 0, ctypes.byref(b), None) == (0 if fits or q_at == out_at else kv.KVIO_EINVAL), kv.kvio_last_error()
+    b.q_out, b.q_out_stride = b.q + 2 * 256, 776                  # strides that differ: by the whole ranges
+    assert lib.kvio_append(h, 0, ctypes.byref(b), None) == kv.KVIO_EINVAL
+    kv.kvio_pool_destroy(h)
+    box.free()
