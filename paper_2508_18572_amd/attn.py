@@ -74,6 +74,13 @@ def _need(ok: bool, text: str) -> None:
         raise _refused(text)
 
 
+def _number(fn: str, name: str, v: int) -> int:
+    """v, which the C struct holds in 32 bits and would cut to its lowest ones."""
+    if not 0 <= v < 1 << 31:
+        raise _refused(f"{fn}: {name} {v} outside [0, 2^31)")
+    return v
+
+
 class Batch:
     """Where the new tokens of several sequences belong (kvio_batch): page_table, int32 (B, max_pages), whose rows
     may lie apart; ctx_len, int32 (B,), the tokens of each context with the new ones; q_start, int32 (B + 1,), the
@@ -96,7 +103,7 @@ class Batch:
         self.device = page_table.device
         _need(all(t is None or t.device == self.device for t in self.tensors), "Batch: tensors on several GPUs")
         self.num_seqs, self._args = B, kvio_batch(
-            B, 0, pages, max_query, stride, page_table.data_ptr(), ctx_len.data_ptr(),
+            B, 0, pages, _number("Batch", "max_query", max_query), stride, page_table.data_ptr(), ctx_len.data_ptr(),
             None if q_start is None else q_start.data_ptr())
 
     def args(self, num_tokens: int) -> kvio_batch:
@@ -139,14 +146,14 @@ def _on(pool, stream, call):
 
 def _cache(fn: str, pool, args, layer: int, like: torch.Tensor) -> None:
     args.dtype = _TYPES[like.dtype]
+    if not 0 <= layer < pool.num_layers:
+        raise _refused(f"{fn}: layer {layer} outside [0, {pool.num_layers})")
     if pool.scales is None:
         _need(pool.tensor.element_size() != 1, f"{fn}: an 8-bit pool needs scales")
         if pool.tensor.dtype != like.dtype:
             raise _refused(f"{fn}: new tokens in {like.dtype}, the pool in {pool.tensor.dtype}")
         args.cache_dtype = args.dtype
         return
-    if not 0 <= layer < pool.num_layers:
-        raise _refused(f"{fn}: layer {layer} outside [0, {pool.num_layers})")
     args.cache_dtype, args.scale_stride = KVIO_E4M3, pool.scales.stride(2)
     args.k_scale, args.v_scale = pool.scales[0, layer].data_ptr(), pool.scales[1, layer].data_ptr()
 
@@ -157,8 +164,9 @@ def append(pool, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor, q: 
     """kvio_append with tensors; see KVPool.append."""
     fn = "append"
     H = pool.tensor.shape[3]
-    a = kvio_append_args(batch=batch.args(k.shape[0]), flags=KVIO_APPEND_INTERLEAVED if interleaved else 0)
+    a = kvio_append_args(flags=KVIO_APPEND_INTERLEAVED if interleaved else 0)
     a.k_stride, a.v_stride = _rows(fn, "k", k, H, pool, None), _rows(fn, "v", v, H, pool, k)
+    a.batch = batch.args(k.shape[0])
     _cache(fn, pool, a, layer, k)
     a.k, a.v = k.data_ptr(), v.data_ptr()
     if inv_freq is not None:
@@ -189,8 +197,9 @@ def attend(pool, layer: int, batch: Batch, q: torch.Tensor, out: Optional[torch.
            workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """kvio_attend with tensors; see KVPool.attend."""
     fn = "attend"
-    a = kvio_attend_args(batch=batch.args(q.shape[0]), num_q_heads=q.shape[1] if q.dim() == 3 else 0, window=window)
+    a = kvio_attend_args(window=_number(fn, "window", window))
     a.q_stride, a.q = _rows(fn, "q", q, None, pool, None), q.data_ptr()
+    a.batch, a.num_q_heads = batch.args(q.shape[0]), q.shape[1]
     _cache(fn, pool, a, layer, q)
     a.softmax_scale = 1.0 / math.sqrt(q.shape[2]) if scale is None else scale
     if lse is not None:
@@ -215,7 +224,8 @@ def attend(pool, layer: int, batch: Batch, q: torch.Tensor, out: Optional[torch.
 def attend_workspace(pool, batch: Batch, q: torch.Tensor, window: int = 0) -> int:
     """Bytes of workspace that attend takes for these; see KVPool.attend."""
     fn = "attend_workspace"
-    a = kvio_attend_args(batch=batch.args(q.shape[0]), num_q_heads=q.shape[1], window=window, softmax_scale=1.0)
+    a = kvio_attend_args(window=_number(fn, "window", window), softmax_scale=1.0)
     _rows(fn, "q", q, None, pool, None)
+    a.batch, a.num_q_heads = batch.args(q.shape[0]), q.shape[1]
     _cache(fn, pool, a, 0, q)
     return kvio_attend_workspace(pool.handle, a)

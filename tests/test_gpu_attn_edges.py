@@ -69,3 +69,23 @@ def test_windows_longer_than_the_context(kv, D, new, bits):  # noqa: F811
     for window in (300 + new, 2 ** 31 - 1):
         assert torch.equal(want, pool.attend(0, batch, g["q"], window=window))
     pool.close()
+
+
+def test_numbers_and_shapes_that_no_call_takes(kv):  # noqa: F811
+    """Numbers that 32 bits do not hold are refused, not cut to their lowest 32 bits; so are tensors of other ranks."""
+    import torch
+    c = filled(16, torch.bfloat16, 4, 2, 64, 16, [(20, 2)], seed=1)
+    g, pool, batch = on_gpu(kv, c)
+    q, k = g["q"], torch.zeros(2, 2, 64, device="cuda", dtype=torch.bfloat16)
+    bad = [lambda: pool.attend(0, batch, q, window=2 ** 32 + 5), lambda: pool.attend(0, batch, q, window=2 ** 31),
+           lambda: pool.attend(2 ** 32, batch, q), lambda: pool.append(2 ** 32, batch, k, k), lambda: pool.attend(-1, batch, q),
+           lambda: kv.Batch(g["table"], g["ctx"], g["starts"], 2 ** 32 + 1), lambda: kv.Batch(g["table"], g["ctx"], g["starts"], -1),
+           lambda: kv.attend_workspace(pool, batch, q, window=2 ** 32), lambda: kv.attend_workspace(pool, batch, q[0]),
+           lambda: kv.attend_workspace(pool, batch, q.sum()), lambda: pool.attend(0, batch, q.sum()), lambda: pool.attend(0, batch, q[0]),
+           lambda: pool.append(0, batch, k.sum(), k), lambda: pool.append(0, batch, k, k.sum()), lambda: pool.append(0, batch, k, k, q=q[0])]
+    for i, f in enumerate(bad):
+        with pytest.raises(kv.KvioError) as e:
+            f()
+        assert e.value.status == kv.KVIO_EINVAL, i
+    pool.attend(0, batch, q, window=2 ** 31 - 1)
+    pool.close()
