@@ -3,7 +3,8 @@
 Like kvio.py it only packs arguments; tensors stand in for pointers.  The calls run on `stream`
 (a torch.cuda.Stream or a raw hipStream_t), or with None on torch's current stream, and allocate
 what they return or need there.  Tensors that a call reads or writes on another stream than their
-own are the caller's to order, as with any kernel.
+own are the caller's to order, as with any kernel.  There is no backward pass: tensors that require
+gradients are refused where autograd records.
 """
 from __future__ import annotations
 
@@ -122,6 +123,8 @@ def _rows(fn: str, name: str, x: torch.Tensor, heads: Optional[int], pool, like:
         raise _refused(f"{fn}: {name} has the type {x.dtype}")
     if like is not None and shape[0] != like.shape[0]:
         raise _refused(f"{fn}: {name} has {shape[0]} tokens, not {like.shape[0]}")
+    if x.requires_grad and torch.is_grad_enabled():
+        raise _refused(f"{fn}: {name} requires gradients and {fn} has no backward pass; call it under torch.no_grad()")
     if x.device != pool.tensor.device:
         raise _refused(f"{fn}: {name} is on {x.device}, the pool on {pool.tensor.device}")
     if stride[2] != 1 or (shape[1] != 1 and stride[1] != D):

@@ -440,7 +440,7 @@ class KVPool:
     """A pool handle over a torch tensor shaped (2, L, S, H, D): K then V, each
     layer a token-major (S, H, D) array of 16-bit or 8-bit elements.
 
-    append and attend take pools of bfloat16, float16 and, with scales, float8_e4m3fn (or
+    append and attend (which have no backward pass) take pools of bfloat16, float16 and, with scales, float8_e4m3fn (or
     uint8 codes): scales is float32 (2, L, S / page_size, H), one for each page
     and head, whose rows of heads may lie apart.
 

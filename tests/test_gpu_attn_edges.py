@@ -89,3 +89,26 @@ def test_numbers_and_shapes_that_no_call_takes(kv):  # noqa: F811
         assert e.value.status == kv.KVIO_EINVAL, i
     pool.attend(0, batch, q, window=2 ** 31 - 1)
     pool.close()
+
+
+def test_tensors_that_want_gradients(kv):  # noqa: F811
+    """Neither call has a backward pass: refused where autograd records, ordinary calls where it does not."""
+    import torch
+    c = filled(16, torch.bfloat16, 4, 2, 64, 16, [(20, 2)], seed=1)
+    g, pool, batch = on_gpu(kv, c)
+    q, k = g["q"], torch.zeros(2, 2, 64, device="cuda", dtype=torch.bfloat16)
+    want = pool.attend(0, batch, q)
+    before = pool.tensor.clone()
+    qg, kg = q.clone().requires_grad_(), k.clone().requires_grad_()
+    for f in (lambda: pool.attend(0, batch, qg), lambda: pool.attend(0, batch, qg * 1.0), lambda: pool.attend(0, batch, q, out=qg),
+              lambda: pool.append(0, batch, kg, k), lambda: pool.append(0, batch, k, kg * 1.0), lambda: pool.append(0, batch, k, k, q=qg)):
+        with pytest.raises(kv.KvioError, match="no backward pass"):
+            f()
+    assert torch.equal(pool.tensor.view(torch.int16), before.view(torch.int16))
+    with torch.no_grad():
+        assert torch.equal(pool.attend(0, batch, qg), want)
+    assert torch.equal(pool.attend(0, batch, (qg * 1.0).detach()), want)
+    with torch.inference_mode():
+        assert torch.equal(pool.attend(0, batch, q.clone()), want)
+    assert not pool.attend(0, batch, q).requires_grad
+    pool.close()
