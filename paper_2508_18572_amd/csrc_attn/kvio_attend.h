@@ -16,10 +16,9 @@ struct Span {
     int32_t lo, hi, whole_lo, whole_hi;
     int32_t tiles;                           // of kTile keys, at multiples of it, that hold [lo, hi)
 };
-// The first key that a row at `place` sees; both may be so far from 0 that 32 bits do not hold their difference.
+// The first key that a row at `place` sees.  Places may be so far below zero that 32 bits do not hold what a window leaves.
 __device__ __forceinline__ int32_t window_from(const AttendArgs &a, int place) {
-    const int64_t from = int64_t(place) - a.window + 1;
-    return a.window > 0 && from > 0 ? static_cast<int32_t>(from) : 0;
+    return a.window > 0 && place >= a.window ? place - a.window + 1 : 0;
 }
 __device__ __forceinline__ Span span_of(const AttendArgs &a, const Seq &s) {
     Span r;
@@ -28,7 +27,8 @@ __device__ __forceinline__ Span span_of(const AttendArgs &a, const Seq &s) {
     r.lo = window_from(a, s.first);
     r.whole_lo = window_from(a, last);
     r.whole_hi = s.first + 1;
-    r.tiles = s.rows > 0 && r.hi > r.lo ? (r.hi + kTile - 1) / kTile - r.lo / kTile : 0;
+    const uint32_t lo = static_cast<uint32_t>(r.lo), hi = static_cast<uint32_t>(r.hi);      // 0 or more, where they count
+    r.tiles = s.rows > 0 && r.hi > r.lo ? static_cast<int32_t>((hi + kTile - 1) / kTile - lo / kTile) : 0;
     return r;
 }
 
@@ -123,7 +123,7 @@ __device__ __forceinline__ void join_partials(int from, int to, int lane, Sums s
 __device__ __forceinline__ void rows_without_keys(const AttendArgs &a, int h, int lane) {
     for (int b = 0; b < a.c.num_seqs; ++b) {
         const Seq s = seq_of(a.c, b);
-        if (s.rows <= 0 || span_of(a, s).tiles != 0) continue;
+        if (s.rows <= 0 || s.first + s.rows > 0) continue;     // the last row's place is not below zero: it sees its own key
         for (int i = 0; i < s.rows * a.group; ++i) {
             const int token = i / a.group, qh = h * a.group + i - token * a.group;
             for (int d = lane; d < a.c.head_dim; d += 64)
