@@ -282,7 +282,11 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     sum[t] += e8[e];
                     if (E4M3) e8[e] *= vs[e];
                 }
-                for (int e = 0; e < 4; ++e) p[t][e] = S::kPBf16 ? pack_bf16(e8[2 * e], e8[2 * e + 1]) : pack_f16(e8[2 * e], e8[2 * e + 1]);
+                for (int e = 0; e < 4; ++e) {
+                    p[t][e] = S::kPBf16 ? pack_bf16(e8[2 * e], e8[2 * e + 1]) : pack_f16(e8[2 * e], e8[2 * e + 1]);
+                    // This value, and no other: rounded once more from a fused product, it differs near ties, and the rest with it.
+                    if constexpr (S::kTwice) keep_here(p[t][e]);
+                }
                 if constexpr (S::kTwice)
                     for (int e = 0; e < 4; ++e) rest[t][e] = pack_f16(e8[2 * e] - f16_lo(p[t][e]), e8[2 * e + 1] - f16_hi(p[t][e]));
             }
