@@ -76,7 +76,7 @@ def exact(c):
 @pytest.mark.parametrize("G,new", [(1, 1), (2, 4), (4, 12), (2, 70), (3, 90)])
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("bits", [8])
+@pytest.mark.parametrize("bits", [8, 16])
 def test_what_probabilities_lose(emu, bits, dtype, D, G, new):  # noqa: F811
     """Half a step of their type, or with a second term (steps, but for bf16 queries over e4m3) half a step of half a step."""
     if new > 16 and D == 256 and bits == 8 and dtype == torch.float16:

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("G,new", [(1, 1), (4, 1), (2, 4), (4, 12), (2, 70), (3, 90)])
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("bits", [8])
+@pytest.mark.parametrize("bits", [8, 16])
 def test_what_probabilities_lose(kv, bits, dtype, D, G, new):  # noqa: F811
     import torch
     dtype = getattr(torch, dtype)
