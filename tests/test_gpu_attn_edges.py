@@ -112,3 +112,26 @@ def test_tensors_that_want_gradients(kv):  # noqa: F811
         assert torch.equal(pool.attend(0, batch, q.clone()), want)
     assert not pool.attend(0, batch, q).requires_grad
     pool.close()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("new", [1, 5, 90])
+def test_pages_outside_the_pool_are_reported(kv, new, bits):  # noqa: F811
+    """By kvio_check, with the sequence and its page, where some row sees a token of theirs; not outside a window or behind a
+    context."""
+    import torch
+    c = filled(bits, torch.bfloat16, 8, 2, 128, 16, [(100, new), (3000, new)], seed=new)
+    g, pool, batch = on_gpu(kv, c)
+    pool.attend(0, batch, g["q"])
+    pool.check()
+    last = (3000 + new - 1) // 16
+    for j, window, seen in ((0, 0, True), (last, 0, True), (last, 10, True), (90, 1000, False), ((3000 - 999) // 16, 1000, True)):
+        keep = g["table"][1, j].item()
+        g["table"][1, j] = -1 if j else 1 << 30
+        pool.attend(0, batch, g["q"], window=window)
+        if seen:
+            with pytest.raises(kv.KvioError, match=f"span 1, context page {j}:"):
+                pool.check()
+        pool.check()
+        g["table"][1, j] = keep
+    pool.close()
