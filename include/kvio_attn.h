@@ -101,8 +101,8 @@ kvio_status kvio_append(kvio_pool_t pool, int32_t layer, const kvio_append_args 
  * of minus infinity; lse[row][h] (if not NULL) is the natural logarithm of the softmax's sum.
  * What hidden tokens hold, infinities and NaN included, has no effect, nor have scales, such ones included, of pages that
  * a row sees no token of (but for the precision that is named below).
- * Products are accumulated in fp32, probabilities rounded to 16 bits for the second one: to the cache's type, with an
- * e4m3 cache to fp16, times their values' scales (a scale below 2^-18 of the context's largest, tokens that the row does
+ * Products are accumulated in fp32, probabilities rounded to 16 bits for the second one: to the cache's type (fp16 in
+ * steps of 2^-31 of the row's largest at least), with an e4m3 cache to fp16, times their values' scales (a scale below 2^-18 of the context's largest, tokens that the row does
  * not see included, loses precision).  With up to 64 rows to a KV head (max_query times query heads; 32 with D of 256) what
  * that takes off is added as a second term (not for bf16 queries over e4m3, whose results do not show it).
  * Equal inputs give equal bits, except over other max_pages, max_query or GPUs.

@@ -10,6 +10,9 @@ constexpr int kTile = 32;                    // keys that a wave takes at a time
 // A running maximum stays until a score passes it by this much (in powers of two): probabilities
 // and their sums stay below 2^8 times the number of keys, and rescaling is rare.
 constexpr float kSlack = 8.0f;
+// fp16 probabilities (beside fp16 values; beside e4m3 ones a ValueUnit does as much) are taken 2^7 times as large, up to 2^15
+// with the slack: steps of 2^-24 are then 2^-31 of the largest, and thousands of small ones beside a large one count.
+template <bool BF16, bool E4M3> constexpr float kRaised = BF16 || E4M3 ? 0.0f : 7.0f;
 
 // The keys of a sequence: those that any row sees, [lo, hi), and those that all see.
 struct Span {

@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                 const float mine = best[t] * unit, now = fmaxf(top[t], fmaxf(mine, lane_xor(mine, 32)));
                 const float less = now == kMinusInf ? 1.0f : exp2_fast(top[t] - now);
                 top[t] = now;
-                from[t] = now == kMinusInf ? 0.0f : now;
+                from[t] = now == kMinusInf ? 0.0f : now - kRaised<BF16, E4M3>;
                 sum[t] *= less;
 #pragma unroll
                 for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                         *reinterpret_cast<u32x2 *>(o + 64 * d + 16 * r + g8) =
                             BF16 ? u32x2{pack_bf16(x0, x1), pack_bf16(x2, x3)} : u32x2{pack_f16(x0, x1), pack_f16(x2, x3)};
                     }
-                if (a.lse != nullptr && g == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top[t], sum[t]);
+                if (a.lse != nullptr && g == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top[t] - kRaised<BF16, E4M3>, sum[t]);
             } else {
                 float *slot = a.partials + block_partial_at(a, worker, from_tile != 0 ? 0 : 1, D);
                 float *o = slot + int64_t(row) * D;
@@ -613,10 +613,11 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + g8 / 2) = f32x4{acc[t][d][4 * r] * by, acc[t][d][4 * r + 1] * by, acc[t][d][4 * r + 2] * by, acc[t][d][4 * r + 3] * by};
-                if (g == 0) *reinterpret_cast<f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row) = f32x2{top[t], sum[t]};
+                if (g == 0) *reinterpret_cast<f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row) = f32x2{top[t] - kRaised<BF16, E4M3>, sum[t]};
             }
         }
-    }    if (a.joined && tid == 0) *my_cut = cut;
+    }
+    if (a.joined && tid == 0) *my_cut = cut;
 }
 
 // Join the partial results of the block that a workgroup was the first to cut, in order, a.join_rows rows to a workgroup.

@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                     sum[t] *= less;
                     for (int d = 0; d < S::kDims; ++d) acc[t][d] *= less;
                 }
-                const float from = top[t] == kMinusInf ? 0.0f : top[t];
+                const float from = top[t] == kMinusInf ? 0.0f : top[t] - kRaised<BF16, E4M3>;
                 float e8[8];
                 for (int e = 0; e < 8; ++e) {
                     e8[e] = exp2_fast(score[e / 4][t][e % 4] - from);
@@ -363,13 +363,13 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
                         const float x = acc[t][d][e] * inv, y = acc[t][d + 1][e] * inv;
                         *reinterpret_cast<uint32_t *>(o + 2 * ((g4 + e) * S::kDims + d)) = BF16 ? pack_bf16(x, y) : pack_f16(x, y);
                     }
-                if (a.lse != nullptr && g == 0) a.lse[int64_t(s.row0 + token) * a.q_heads + qh] = lse_of(top[t], sum[t]);
+                if (a.lse != nullptr && g == 0) a.lse[int64_t(s.row0 + token) * a.q_heads + qh] = lse_of(top[t] - kRaised<BF16, E4M3>, sum[t]);
             } else {
                 // Which of the two contexts that a range can share with others: the one that began before it, or the one that goes on.
                 float *o = a.partials + partial_at(a, worker, h, at != seq_begin ? 0 : 1, row, D);
                 for (int e = 0; e < 4; ++e)
                     for (int d = 0; d < S::kDims; ++d) o[(g4 + e) * S::kDims + d] = E4M3 ? acc[t][d][e] * unit.unit : acc[t][d][e];
-                if (g == 0) o[D] = top[t], o[D + 1] = sum[t];
+                if (g == 0) o[D] = top[t] - kRaised<BF16, E4M3>, o[D + 1] = sum[t];
             }
         }
         at = stop;

@@ -96,3 +96,32 @@ def test_what_probabilities_lose(emu, bits, dtype, D, G, new):  # noqa: F811
     bad = ~((out.double() - want).abs() <= tol)[:N]
     assert not bool(bad.any()), (int(bad.sum()), bad.numel())
     assert said is None and bool((out[N:] == -2.5).all())
+
+
+@pytest.mark.parametrize("new,window", [(1, 0), (12, 0), (90, 0), (90, 350)])
+def test_small_fp16_probabilities_that_add_up(emu, new, window):  # noqa: F811
+    """One token takes nearly all of a row's probability, its value is small; hundreds that have 2^-27 of it and large values
+    make the result."""
+    c = case(torch.float16, 16, 1, 2, 64, 16, [(400, new)], window=window, seed=new)
+    c["max_query"] = new
+    ctx = 400 + new
+    place = torch.arange(ctx)
+    slots = c["table"][0, place // 16].long() * 16 + place % 16
+    gen = torch.Generator().manual_seed(1)
+    c["pool"][0, slots] = 0
+    c["pool"][1, slots] = (1000 + torch.rand(ctx, 1, 64, generator=gen) * 500).half()
+    strong = slots[max(0, ctx - new - 30)]                          # in every row's window
+    c["pool"][0, strong, 0, 0], c["pool"][1, strong] = 8, 2.0 ** -10
+    c["q"][:] = 0
+    c["q"][..., 0] = 27 * math.log(2)                               # times 8 / sqrt(64)
+    out, lse, _ = call(emu, c)
+    k, v = c["pool"][0, slots, 0].double(), c["pool"][1, slots, 0].double()
+    for i in range(new):
+        seen = torch.arange(max(0, 400 + i - window + 1) if window else 0, 400 + i + 1)
+        s = k[seen] @ c["q"][i, 0].double() / 8
+        p = torch.softmax(s, 0)
+        want = p @ v[seen]
+        # a probability is exact here but for half a step of fp16, its exponent's error (2^-24 of 27), and 2^-32 of the largest
+        tol = want * (2 * STEP[torch.float16] + 27 * 2.0 ** -23 + len(seen) * 2.0 ** -23) + len(seen) * 2.0 ** -32 * 1500 + 2.0 ** -25
+        assert bool(((out[i].double() - want).abs() <= tol).all()), (i, out[i, 0, :3], want[:3])
+        assert abs(float(lse[i, 0]) - float(torch.logsumexp(s, 0))) <= 2.0 ** -18
