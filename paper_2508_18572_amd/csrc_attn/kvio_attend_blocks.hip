@@ -2,17 +2,21 @@
 // and the rest of partly cached ones), on the matrix units.
 //
 // A workgroup takes a block of 256 rows (128 with heads of 256 dims), query heads
-// and tokens of one KV head, 64 (32) to a wave, and goes through its keys a tile at a time.  Rows are columns of
-// both products,
+// and tokens of one KV head, 32 to a wave, and goes through its keys 64 at a time.
+// Rows are columns of both products,
 //   scores^T (keys x rows) = K Q^T,  out^T (dims x rows) += V^T probabilities^T,
 // so that the scores that a lane gets are the probabilities that it has to bring
 // to the second product, and a row's maximum and sum concern two lanes.  Q and
 // out^T stay in registers; K and V come from the pages through registers, where
-// codes are widened to 16 bits, into LDS buffers shared by the four waves, a tile ahead.  V^T is read with the LDS' transposing loads.
+// codes are widened to 16 bits, into LDS buffers that all waves share, a tile
+// ahead.  V^T is read with the LDS' transposing loads.
 //
-// 4 D flops to a score against some six vector operations: both units have to be
-// kept busy at once.  A wave's 512 registers hold the scores of two tiles, so
-// that the products of the next tile's run beside the exponentials of this one's.
+// 4 D flops to a score against some eight vector operations: both units have to be
+// kept busy at once.  Eight waves, two to a SIMD with 256 registers each, fill each
+// other's gaps, and a wave's registers hold the scores of two halves of a tile, so
+// that the products of the next half's run beside the exponentials of this one's
+// (8192 tokens of 32 heads, 128 dims: four waves of 64 rows 904 us, eight of 32
+// 792 us).  Heads of 256 dims leave room for four waves, one to a SIMD.
 //
 // Work is split over all blocks' keys, laid end to end, in equal ranges, one to a
 // workgroup: ragged batches and causal triangles load the GPU evenly.  A block
@@ -138,7 +142,8 @@ struct Shape {
     static constexpr int kElem = E4M3 ? 1 : 2, kSeg = D * kElem;
     static constexpr int kKeys = 64;                     // of a tile
     static constexpr int kWaves = waves_of(D), kThreads = 64 * kWaves;
-    static constexpr int kWaveRows = block_rows(D) / kWaves, kColumns = kWaveRows / 32;   // rows to a wave, 32 to a column of products
+    static constexpr int kWaveRows = 32;                 // rows to a wave, columns of its products
+    static_assert(kWaveRows * kWaves == block_rows(D));
     static constexpr int kSteps = D / 16, kDimBlocks = D / 32;
     static constexpr int kPieces = kSeg / 16, kRowsAtOnce = std::min(kKeys, kThreads / kPieces), kPasses = kKeys / kRowsAtOnce;
     // 16 rows' pieces of 16 bytes lie in all banks; so do 32 bytes of 8 rows
@@ -148,6 +153,9 @@ struct Shape {
     // 64 bits of 0.0022 -> 0.0017 of the result's norm; windowed prompts of 256 dims in fp16: 156 -> 178 us, 0.00029 -> 0.00021).
     static constexpr bool kPBf16 = BF16 && !E4M3;
     // Operands in registers at a time; with fewer than a phase has, K of a tile is still read while the next but one is put.
+    // As many as the registers last for: over e4m3 with 128 dims, four of K spill.  Three of V, not two: 676 against 679 us for
+    // 8192 tokens of 32 heads, 128 dims, 504 against 509 us for two prompts of 3500 tokens, 16 heads of 256 dims over e4m3 (eight
+    // instead of all); four change nothing.
     static constexpr int kKOps = D == 128 && E4M3 ? 2 : D <= 128 ? 4 : kSteps, kVOps = D <= 128 ? 3 : 2 * kDimBlocks, kKBuffers = kKOps < kSteps ? 3 : 2;
     struct alignas(16) Lds {
         uint8_t k[kKBuffers][kKeys * kKRow], v[2][kKeys * kVRow];
@@ -159,7 +167,7 @@ struct Shape {
 template <bool BF16, bool E4M3, int D>
 __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_blocks(const AttendArgs a) {
     using S = Shape<BF16, E4M3, D>;
-    constexpr int kKeys = S::kKeys, kColumns = S::kColumns, kWaveRows = S::kWaveRows;
+    constexpr int kKeys = S::kKeys, kWaveRows = S::kWaveRows;
     __shared__ typename S::Lds lds;
     const CacheArgs &c = a.c;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = wave_first(tid >> 6);
@@ -213,27 +221,22 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
 
         int g16 = 16 * g;
         keep_here(g16);
-        int place[kColumns];                             // of the lane's columns; below any key for none
-        u32x4 q[kColumns][S::kSteps];
-#pragma unroll
-        for (int t = 0; t < kColumns; ++t) {
-            const int row = wave_row0 + 32 * t + m, token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div));
-            place[t] = row < rows ? first + token : -1;
+        // The lane's column is one row: its place, below any key for none.
+        int place;
+        u32x4 q[S::kSteps];
+        {
+            const int row = wave_row0 + m, token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div));
+            place = row < rows ? first + token : -1;
             const uint8_t *p = a.q + (s.row0 + block_row0 + token) * a.q_stride + int64_t(h * a.group + row - token * a.group) * (2 * D) + g16;
 #pragma unroll
-            for (int i = 0; i < S::kSteps; ++i) q[t][i] = row < rows ? *reinterpret_cast<const u32x4 *>(p + 32 * i) : u32x4{0, 0, 0, 0};
+            for (int i = 0; i < S::kSteps; ++i) q[i] = row < rows ? *reinterpret_cast<const u32x4 *>(p + 32 * i) : u32x4{0, 0, 0, 0};
         }
-        f32x16 acc[kColumns][S::kDimBlocks];
-        float top[kColumns], sum[kColumns];
+        f32x16 acc[S::kDimBlocks];
+        float top = kMinusInf, sum = 0;
 #pragma unroll
-        for (int t = 0; t < kColumns; ++t) {
+        for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll
-            for (int d = 0; d < S::kDimBlocks; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[t][d][i] = 0;
-            top[t] = kMinusInf;
-            sum[t] = 0;
-        }
+            for (int i = 0; i < 16; ++i) acc[d][i] = 0;
 
         // ---- keys and values on their way into LDS ----------------------------------------
         auto page_in = [&](int tile) KVIO_INLINE {       // of the lane's key; some page for one that no row sees
@@ -268,11 +271,9 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             float vs_now = is_there ? v_scale : 0.0f;
             bool odd;
             const float less = value_unit.take(vs_now, odd);
-            if (less != 1.0f) {                          // rare, and the same in all waves: what is in the old unit follows
+            if (__builtin_expect(less != 1.0f, 0)) {                          // rare, and the same in all waves: what is in the old unit follows
 #pragma unroll
-                for (int t = 0; t < kColumns; ++t)
-#pragma unroll
-                    for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
+                for (int d = 0; d < S::kDimBlocks; ++d) acc[d] *= less;
                 vs[0] *= less, vs[1] *= less;
                 workgroup_barrier();
                 if (wave < 4) lds.v_scale[wave][lane] *= less;
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             for (int i = 0; i < S::kPasses; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) any.look(vx[i][e]);
-            if (!wave_any(any.found())) return;
+            if (__builtin_expect(!wave_any(any.found()), 1)) return;
 #pragma unroll
             for (int i = 0; i < S::kPasses; ++i)
 #pragma unroll
@@ -338,9 +339,9 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
 
         // ---- products, 32 keys at a time: half i of a tile ---------------------------------
         // Scores (of keys 8 (e / 4) + 4 g + e % 4) become probabilities, and take part in the maximum, in units of two.
-        constexpr int kUnits = 8 * kColumns, kScoreProducts = S::kSteps * kColumns, kOutProducts = 2 * S::kDimBlocks * kColumns;
-        f32x16 score[kColumns], ahead[kColumns];
-        u32x4 k_op[S::kKOps], v_op[S::kVOps], p[kColumns][2];
+        constexpr int kUnits = 8, kScoreProducts = S::kSteps, kOutProducts = 2 * S::kDimBlocks;
+        f32x16 score, ahead;
+        u32x4 k_op[S::kKOps], v_op[S::kVOps], p[2];
         auto fetch_k = [&](int buffer, int i, int e) KVIO_INLINE {
             k_op[e % S::kKOps] = *reinterpret_cast<const u32x4 *>(lds.k[buffer] + (32 * i + m) * S::kKRow + 16 * g + 32 * e);
         };
@@ -353,66 +354,56 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         auto fetch_scales = [&](f32x4 *to, const float *scales, int i, int r) KVIO_INLINE {
             if constexpr (E4M3) to[r % 2] = *reinterpret_cast<const f32x4 *>(scales + 32 * i + 8 * r + 4 * g);
         };
-        auto score_product = [&](int i, f32x16 (&x)[kColumns]) KVIO_INLINE {
-            const int e = i / kColumns, t = i % kColumns;
+        auto score_product = [&](int i, f32x16 &x) KVIO_INLINE {
             const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-            x[t] = product32<BF16>(k_op[e % S::kKOps], q[t][e], e == 0 ? zero : x[t]);
+            x = product32<BF16>(k_op[i % S::kKOps], q[i], i == 0 ? zero : x);
         };
         auto out_product = [&](int i) KVIO_INLINE {
-            const int e = i / kColumns, t = i % kColumns, u = e / S::kDimBlocks, d = e % S::kDimBlocks;
-            acc[t][d] = product32<S::kPBf16>(v_op[e % S::kVOps], p[t][u], acc[t][d]);
+            const int u = i / S::kDimBlocks, d = i % S::kDimBlocks;
+            acc[d] = product32<S::kPBf16>(v_op[i % S::kVOps], p[u], acc[d]);
         };
         // Scores are in powers of two once multiplied by `unit`.
         const float unit = E4M3 ? 1.0f : a.scale_log2;
-        float best[kColumns], from[kColumns];            // of a half; what is taken off a score: the maximum, or 0 where there is none
-        auto largest = [&](int i, f32x16 (&x)[kColumns]) KVIO_INLINE {
-            const int t = i % kColumns, e = i / kColumns * 2;
-            if (E4M3) x[t][e] *= ks[e / 4 % 2][e % 4], x[t][e + 1] *= ks[e / 4 % 2][e % 4 + 1];
-            const float of_two = larger(x[t][e], x[t][e + 1]);
-            best[t] = e == 0 ? of_two : larger(best[t], of_two);
-            if (e == 14) keep_here(best[t]);
+        float best, from = 0;                            // of a half; what is taken off a score: the maximum, or 0 where there is none
+        auto largest = [&](int i, f32x16 &x) KVIO_INLINE {
+            const int e = 2 * i;
+            if (E4M3) x[e] *= ks[e / 4 % 2][e % 4], x[e + 1] *= ks[e / 4 % 2][e % 4 + 1];
+            const float of_two = larger(x[e], x[e + 1]);
+            best = e == 0 ? of_two : larger(best, of_two);
+            if (e == 14) keep_here(best);
         };
-        auto probability = [&](int i, const f32x16 (&x)[kColumns]) KVIO_INLINE {
-            const int t = i % kColumns, e = i / kColumns * 2;
-            float y = exp2_fast(fmaf(x[t][e], unit, -from[t])), z = exp2_fast(fmaf(x[t][e + 1], unit, -from[t]));
-            sum[t] += y + z;
-            if (e == 14) keep_here(sum[t]);
+        auto probability = [&](int i, const f32x16 &x) KVIO_INLINE {
+            const int e = 2 * i;
+            float y = exp2_fast(fmaf(x[e], unit, -from)), z = exp2_fast(fmaf(x[e + 1], unit, -from));
+            sum += y + z;
+            if (e == 14) keep_here(sum);
             if (E4M3) y *= vs[e / 4 % 2][e % 4], z *= vs[e / 4 % 2][e % 4 + 1];
-            p[t][e / 8][e / 2 % 4] = S::kPBf16 ? pack_bf16(y, z) : pack_f16(y, z);
+            p[e / 8][e / 2 % 4] = S::kPBf16 ? pack_bf16(y, z) : pack_f16(y, z);
         };
-        auto mask = [&](int tile, int i, uint64_t there, f32x16 (&x)[kColumns]) KVIO_INLINE { // hidden keys at minus infinity
+        auto mask = [&](int tile, int i, uint64_t there, f32x16 &x) KVIO_INLINE { // hidden keys at minus infinity
             const int base = base0 + tile * kKeys + 32 * i;
             if (idle || (base + 31 <= wave_first_place && (a.window == 0 || base > wave_last_place - a.window) && there == ~0ull)) return;
             // Bit n of `seen`: the row sees key base + 4 g + n.
             const uint32_t mine = static_cast<uint32_t>(there >> (32 * i + 4 * g));
+            const int up_to = place - (base + 4 * g);
+            uint32_t seen = mine & low_bits(up_to);
+            if (a.window > 0) seen &= ~low_bits(place < 0 ? -1 : up_to - a.window);
+            best = kMinusInf;
 #pragma unroll
-            for (int t = 0; t < kColumns; ++t) {
-                const int up_to = place[t] - (base + 4 * g);
-                uint32_t seen = mine & low_bits(up_to);
-                if (a.window > 0) seen &= ~low_bits(place[t] < 0 ? -1 : up_to - a.window);
-                best[t] = kMinusInf;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    x[t][e] = where_bit(seen, 8 * (e / 4) + e % 4, x[t][e], kMinusInf);
-                    best[t] = larger(best[t], x[t][e]);
-                }
+            for (int e = 0; e < 16; ++e) {
+                x[e] = where_bit(seen, 8 * (e / 4) + e % 4, x[e], kMinusInf);
+                best = larger(best, x[e]);
             }
         };
         auto raise = [&]() KVIO_INLINE {                 // a new maximum where the old one is passed by far
-            bool any = false;
+            if (!wave_any(best * unit > top + kSlack)) return;
+            const float mine = best * unit, now = fmaxf(top, fmaxf(mine, lane_xor(mine, 32)));
+            const float less = now == kMinusInf ? 1.0f : exp2_fast(top - now);
+            top = now;
+            from = now == kMinusInf ? 0.0f : now - kRaised<BF16, E4M3>;
+            sum *= less;
 #pragma unroll
-            for (int t = 0; t < kColumns; ++t) any = any || best[t] * unit > top[t] + kSlack;
-            if (!wave_any(any)) return;
-#pragma unroll
-            for (int t = 0; t < kColumns; ++t) {
-                const float mine = best[t] * unit, now = fmaxf(top[t], fmaxf(mine, lane_xor(mine, 32)));
-                const float less = now == kMinusInf ? 1.0f : exp2_fast(top[t] - now);
-                top[t] = now;
-                from[t] = now == kMinusInf ? 0.0f : now - kRaised<BF16, E4M3>;
-                sum[t] *= less;
-#pragma unroll
-                for (int d = 0; d < S::kDimBlocks; ++d) acc[t][d] *= less;
-            }
+            for (int d = 0; d < S::kDimBlocks; ++d) acc[d] *= less;
         };
         // Rare: values that are not finite reach the rows that see them, and no others.
         auto add_odd = [&](int tile) KVIO_INLINE {
@@ -432,9 +423,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                         const float f = element<BF16, E4M3>(v, 32 * d + 8 * (e / 4) + 4 * g + e % 4) * by;
                         in_order();
                         if (!wave_any(f - f != 0)) continue;
-#pragma unroll
-                        for (int t = 0; t < kColumns; ++t)
-                            acc[t][d][e] += f - f != 0 && key <= place[t] && (a.window == 0 || key > place[t] - a.window) ? f : 0.0f;
+                        acc[d][e] += f - f != 0 && key <= place && (a.window == 0 || key > place - a.window) ? f : 0.0f;
                     }
             }
         };
@@ -486,18 +475,16 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
 #pragma unroll
             for (int i = 0; i < kScoreProducts; ++i) {
                 score_product(i, score);
-                if (i % kColumns == kColumns - 1 && i / kColumns + S::kKOps < S::kSteps) fetch_k(0, 0, i / kColumns + S::kKOps);
+                if (i + S::kKOps < S::kSteps) fetch_k(0, 0, i + S::kKOps);
             }
 #pragma unroll
             for (int e = 0; e < S::kKOps; ++e) fetch_k(0, 1, e);
             fetch_scales(vs, lds.v_scale[0], 0, 0);
 #pragma unroll
             for (int i = 0; i < kUnits; ++i) {
-                if (i % (2 * kColumns) == 0) fetch_scales(ks, lds.k_scale[0], 0, i / (2 * kColumns));
+                if (i % 2 == 0) fetch_scales(ks, lds.k_scale[0], 0, i / 2);
                 largest(i, score);
             }
-#pragma unroll
-            for (int t = 0; t < kColumns; ++t) from[t] = 0;
             mask(0, 0, there0, score);
             raise();
         }
@@ -505,7 +492,8 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         // Each half in two phases: the next half's scores beside this one's probabilities, then this one's part of out^T
         // beside the next half's maximum.  Operands are fetched, and tiles moved on, one phase or more before they are
         // used, a little beside each product: a matrix product takes as long as 8 other instructions, and the compiler,
-        // left to itself, puts all of one kind first (8192 tokens of 32 heads, 128 dims: 912 us).
+        // left to itself, puts all of one kind first (8192 tokens of 32 heads, 128 dims: 912 us).  What is rare is said to be
+        // (__builtin_expect): its code then lies behind the loop, not in it (windowed prompts of 256 dims 157 -> 147 us).
         int k0 = 0;                                      // where K of tile j lies
         for (int j = 0; j < n; ++j) {
             const int k1 = k0 + 1 == S::kKBuffers ? 0 : k0 + 1, k2 = k1 + 1 == S::kKBuffers ? 0 : k1 + 1;
@@ -513,7 +501,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             put_scales(j + 3, there3);
             const int page5 = page_in(j + 5);            // before the tiles' loads, so that waiting for it does not wait for them
             in_order();
-            auto scores_phase = [&](int half, const f32x16 (&now)[kColumns], f32x16 (&next)[kColumns]) KVIO_INLINE {
+            auto scores_phase = [&](int half, const f32x16 &now, f32x16 &next) KVIO_INLINE {
 #pragma unroll
                 for (int i = 0; i < kScoreProducts; ++i) {
                     score_product(i, next);
@@ -525,16 +513,16 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                     }
 #pragma unroll
                     for (int e = i * S::kVOps / kScoreProducts; e < (i + 1) * S::kVOps / kScoreProducts; ++e) fetch_v(j, half, e);
-                    if (i % kColumns == kColumns - 1 && i / kColumns + S::kKOps < S::kSteps) fetch_k(half == 0 ? k0 : k1, 1 - half, i / kColumns + S::kKOps);
+                    if (i + S::kKOps < S::kSteps) fetch_k(half == 0 ? k0 : k1, 1 - half, i + S::kKOps);
 #pragma unroll
                     for (int e = i * kUnits / kScoreProducts; e < (i + 1) * kUnits / kScoreProducts; ++e) {
-                        if (e % (2 * kColumns) == 0 && e < 6 * kColumns) fetch_scales(vs, lds.v_scale[j & 3], half, e / (2 * kColumns) + 1);
+                        if (e % 2 == 0 && e < 6) fetch_scales(vs, lds.v_scale[j & 3], half, e / 2 + 1);
                         probability(e, now);
                     }
                     in_order();
                 }
             };
-            auto out_phase = [&](int half, f32x16 (&next)[kColumns]) KVIO_INLINE {
+            auto out_phase = [&](int half, f32x16 &next) KVIO_INLINE {
 #pragma unroll
                 for (int i = 0; i < kOutProducts; ++i) {
                     out_product(i);
@@ -546,13 +534,13 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
                     }
 #pragma unroll
                     for (int e = i * S::kKOps / kOutProducts; e < (i + 1) * S::kKOps / kOutProducts; ++e) fetch_k(k1, half, e);
-                    if (i % kColumns == kColumns - 1 && i / kColumns + S::kVOps < 2 * S::kDimBlocks) fetch_v(j, half, i / kColumns + S::kVOps);
+                    if (i + S::kVOps < 2 * S::kDimBlocks) fetch_v(j, half, i + S::kVOps);
                     // not beside the first ones: the next scores are just being finished
                     constexpr int kLate = kOutProducts / 4;
                     if (i >= kLate)
 #pragma unroll
                         for (int e = (i - kLate) * kUnits / (kOutProducts - kLate); e < (i + 1 - kLate) * kUnits / (kOutProducts - kLate); ++e) {
-                            if (e % (2 * kColumns) == 0 && e < 6 * kColumns) fetch_scales(ks, lds.k_scale[(j + half) & 3], 1 - half, e / (2 * kColumns) + 1);
+                            if (e % 2 == 0 && e < 6) fetch_scales(ks, lds.k_scale[(j + half) & 3], 1 - half, e / 2 + 1);
                             largest(e, next);
                         }
                     in_order();
@@ -567,7 +555,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
             in_order();
             scores_phase(1, ahead, score);
             out_phase(1, score);
-            if (lds.odd[(serial + j) & 3] == serial + j) add_odd(j);   // before the maximum moves
+            if (__builtin_expect(lds.odd[(serial + j) & 3] == serial + j, 0)) add_odd(j);   // before the maximum moves
             mask(j + 1, 0, there1, score);
             raise();
             const int slot4 = slot_from(j + 4, page4);
@@ -582,39 +570,36 @@ __global__ void __launch_bounds__(64 * waves_of(D), waves_of(D) / 4) attend_bloc
         serial += n;
 
         const bool alone = n == all_tiles;
-        int g8 = 8 * g;                                  // computed here, not kept from block to block
+        sum += lane_xor(sum, 32);
+        int g8 = 8 * g, last_m = m;                      // computed here, not kept from block to block where registers are short
         keep_here(g8);
+        if constexpr (D > 64) keep_here(last_m);
+        const int out_row = wave_row0 + last_m;
+        if (out_row < rows && alone) {
+            const int token = static_cast<int>(div_by(static_cast<uint32_t>(out_row), a.group_div)), qh = h * a.group + out_row - token * a.group;
+            const float inv = sum == 0 ? 0.0f : (E4M3 ? value_unit.unit : 1.0f) / sum;
+            const int64_t array_row = s.row0 + block_row0 + token;
+            uint8_t *o = a.out + array_row * a.out_stride + int64_t(qh) * (2 * D);
 #pragma unroll
-        for (int t = 0; t < kColumns; ++t) {
-            sum[t] += lane_xor(sum[t], 32);
-            const int row = wave_row0 + 32 * t + m;
-            if (row >= rows) continue;
-            if (alone) {
-                const int token = static_cast<int>(div_by(static_cast<uint32_t>(row), a.group_div)), qh = h * a.group + row - token * a.group;
-                const float inv = sum[t] == 0 ? 0.0f : (E4M3 ? value_unit.unit : 1.0f) / sum[t];
-                const int64_t array_row = s.row0 + block_row0 + token;
-                uint8_t *o = a.out + array_row * a.out_stride + int64_t(qh) * (2 * D);
+            for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll
-                for (int d = 0; d < S::kDimBlocks; ++d)
+                for (int r = 0; r < 4; ++r) {
+                    const f32x16 &x = acc[d];
+                    const float x0 = x[4 * r] * inv, x1 = x[4 * r + 1] * inv, x2 = x[4 * r + 2] * inv, x3 = x[4 * r + 3] * inv;
+                    *reinterpret_cast<u32x2 *>(o + 64 * d + 16 * r + g8) =
+                        BF16 ? u32x2{pack_bf16(x0, x1), pack_bf16(x2, x3)} : u32x2{pack_f16(x0, x1), pack_f16(x2, x3)};
+                }
+            if (a.lse != nullptr && g == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top - kRaised<BF16, E4M3>, sum);
+        } else if (out_row < rows) {
+            float *slot = a.partials + block_partial_at(a, worker, from_tile != 0 ? 0 : 1, D);
+            float *o = slot + int64_t(out_row) * D;
+            const float by = E4M3 ? value_unit.unit : 1.0f;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const f32x16 &x = acc[t][d];
-                        const float x0 = x[4 * r] * inv, x1 = x[4 * r + 1] * inv, x2 = x[4 * r + 2] * inv, x3 = x[4 * r + 3] * inv;
-                        *reinterpret_cast<u32x2 *>(o + 64 * d + 16 * r + g8) =
-                            BF16 ? u32x2{pack_bf16(x0, x1), pack_bf16(x2, x3)} : u32x2{pack_f16(x0, x1), pack_f16(x2, x3)};
-                    }
-                if (a.lse != nullptr && g == 0) a.lse[array_row * a.q_heads + qh] = lse_of(top[t] - kRaised<BF16, E4M3>, sum[t]);
-            } else {
-                float *slot = a.partials + block_partial_at(a, worker, from_tile != 0 ? 0 : 1, D);
-                float *o = slot + int64_t(row) * D;
-                const float by = E4M3 ? value_unit.unit : 1.0f;
+            for (int d = 0; d < S::kDimBlocks; ++d)
 #pragma unroll
-                for (int d = 0; d < S::kDimBlocks; ++d)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + g8 / 2) = f32x4{acc[t][d][4 * r] * by, acc[t][d][4 * r + 1] * by, acc[t][d][4 * r + 2] * by, acc[t][d][4 * r + 3] * by};
-                if (g == 0) *reinterpret_cast<f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * row) = f32x2{top[t] - kRaised<BF16, E4M3>, sum[t]};
-            }
+                for (int r = 0; r < 4; ++r)
+                    *reinterpret_cast<f32x4 *>(o + 32 * d + 8 * r + g8 / 2) = f32x4{acc[d][4 * r] * by, acc[d][4 * r + 1] * by, acc[d][4 * r + 2] * by, acc[d][4 * r + 3] * by};
+            if (g == 0) *reinterpret_cast<f32x2 *>(slot + int64_t(a.slot_rows) * D + 2 * out_row) = f32x2{top - kRaised<BF16, E4M3>, sum};
         }
     }
     if (a.joined && tid == 0) *my_cut = cut;
@@ -681,7 +666,9 @@ AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_b
     p.groups = static_cast<uint32_t>((workers + 7) / 8 * 8);
     p.workers = static_cast<int32_t>(p.groups);
     p.joined = workers > 1;
-    p.join_rows = blocks <= 64 ? 4 : 16;                 // few blocks have many partial results each
+    // Few blocks have many partial results each: 100 tokens behind 16384 of 32 heads take 64 us with 4 rows to a workgroup, 81
+    // with 16; a prompt of 8192 tokens 705 and 700 us.
+    p.join_rows = blocks <= 64 ? 4 : 16;
     p.slot_rows = static_cast<int32_t>(std::min<int64_t>(p.block_tokens, max_query) * group + 1) & ~1;
     if (p.joined) p.bytes = uint64_t(p.workers) * (sizeof(Cut) + 2 * uint64_t(p.slot_rows) * uint64_t(dim + 2) * 4);
     return p;

@@ -25,7 +25,9 @@ namespace kvio {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kFewRows = 512;                  // rows and query heads, below which each is joined by 16 waves
+// Rows times query heads up to which each is joined by 16 waves: few have many partial results each.  One context of 131072
+// tokens, 32 heads: 61 us, with one wave 108; 160 rows of 64 heads (5 drafts of 32 contexts): one wave 104 us, 16 174.
+constexpr int kFewRows = 512;
 
 // A wave's slots and scales of two tiles, and its rows of Q.
 template <int D, int NT>
@@ -35,7 +37,7 @@ struct alignas(16) WaveLds {
     uint8_t q[16 * NT][2 * D + 16];          // 16 more, so that 16 rows' pieces lie in all banks
 };
 
-// Waves to a SIMD for which the registers last without scratch.
+// Waves to a SIMD for which the registers last without scratch, found by compiling for more.
 constexpr int occupancy(bool e4m3, int dim, int columns) {
     return dim * columns <= 64 ? 4 : dim * columns <= 128 ? 3 : dim * columns <= 256 && (dim == 64 ? columns < 4 : e4m3 || dim == 128) ? 2 : 1;
 }
@@ -159,7 +161,8 @@ __global__ void __launch_bounds__(kThreads, occupancy(E4M3, D, NT)) attend_steps
             for (int i = g; i < D / 8; i += 4)
                 *reinterpret_cast<u32x4 *>(keys.q[row] + 16 * i) = row < rows ? *reinterpret_cast<const u32x4 *>(p + 16 * i) : u32x4{0, 0, 0, 0};
         }
-        // A SIMD's only wave has the registers to keep Q's operands, and nobody to work while it waits for LDS.
+        // A SIMD's only wave has the registers to keep Q's operands, and nobody to work while it waits for LDS: 8 drafts of 4
+        // heads 43.6 us, with Q read from LDS each time 44.5; 4 of 4 with 256 dims 47.4 and 49.9; but 5 of 8 over e4m3 104 and 102.
         constexpr bool kKeepQ = occupancy(E4M3, D, NT) == 1;
         u32x4 q[kKeepQ ? NT : 1][kKeepQ ? S::kSteps : 1];
         auto q_operand = [&](int t, int s2) __attribute__((always_inline)) {

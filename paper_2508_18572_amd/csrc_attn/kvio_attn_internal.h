@@ -65,7 +65,7 @@ struct AttendPlan {
     bool joined;                   // partial results may be left
     uint64_t bytes;
 };
-// Rows that a workgroup of kvio_attend_blocks.hip holds: out^T of a wave's share takes half the registers.
+// Rows that a workgroup of kvio_attend_blocks.hip holds, 32 to a wave: out^T of these takes D / 2 of a lane's registers.
 constexpr int block_rows(int dim) { return dim <= 128 ? 256 : 128; }
 AttendPlan plan_steps(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
 AttendPlan plan_blocks(int32_t heads, int32_t q_heads, int32_t dim, const kvio_batch &b, int32_t max_query, int32_t max_ctx);
