@@ -40,8 +40,10 @@ extern "C" {
  * ctx_len[b] - 1 - j.  Context token t lives in pool slot
  * page_table[b][t / P] * P + t % P.
  * Values that make no sense are cut to what is there: offsets to [0,
- * num_tokens] and to the one before, lengths to [0, max_pages * P], new tokens
- * to the first max_query.  A row whose place comes out below zero, or whose page lies
+ * num_tokens], lengths to [0, max_pages * P], new tokens
+ * to the first max_query.  Offsets must not fall: a sequence that ends before it begins has no rows, and it is not
+ * defined which of the rows that the others name are worked on then, nor for which; no other rows or pages are
+ * touched.  A row whose place comes out below zero, or whose page lies
  * outside the pool, is not appended; a cached token whose page lies outside the
  * pool is attended by nobody.  The first such page is reported by kvio_check
  * (span = the sequence). */

@@ -23,7 +23,8 @@ FLAGS = [
     "-Wall", "-Wextra", "-Werror", "-Wno-unused-parameter",
     # keep the compiler from forming packed fp32 ops
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # matrix products in either kind of registers: attention reads their results with ordinary instructions
+    # matrix products in either kind of registers: attention reads their results with ordinary instructions (the
+    # transfer kernels, which have no such products, come out the same with and without it)
     "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-I", INCLUDE, "-I", CSRC, "-I", os.path.join(PKG, "csrc_attn"), "-pthread",
 ]

@@ -167,3 +167,45 @@ def test_slices_of_one_buffer(emu, q_at, out_at, fits):  # noqa: F811
     assert lib.kvio_append(h, 0, ctypes.byref(b), None) == kv.KVIO_EINVAL
     kv.kvio_pool_destroy(h)
     box.free()
+
+
+@pytest.mark.parametrize("starts", [[0, 5, 3, 8], [0, 90, 1, 2], [6, 2, 90, 40], [90, 90, 0, 90], [-5, 200, -7, 3], [2 ** 31 - 1, -2 ** 31, 0, 90]])
+@pytest.mark.parametrize("bits", [8, 16])
+def test_falling_offsets_touch_nothing_else(emu, bits, starts):  # noqa: F811
+    """Which rows such a call works on is not defined; rows, slots and scales of no sequence stay, every access is in bounds (the
+    buffers lie against inaccessible pages), and the call ends."""
+    kv, lib, A = emu
+    N, P, H, D = 92, 16, 2, 64
+    for max_query in (0, 12):
+        c = case(torch.bfloat16, bits, H, 2, D, P, [(10, 80), (0, 95), (30, 60)], seed=5)
+        c["q"], c["q_out"] = c["q"][:N].contiguous(), c["q_out"][:N].contiguous()
+        c["max_query"] = max_query
+        box = Box(kv)
+        pool, h = make_pool(kv, box, c)
+        batch = batch_args(A, box, c, c["table"], c["ctx"], torch.tensor(starts, dtype=torch.int32), N, max_query)
+        a = A.kvio_attend_args(batch=batch, dtype=0, cache_dtype=2 if bits == 8 else 0, num_q_heads=4, softmax_scale=0.125, q_stride=256, out_stride=256)
+        b = A.kvio_append_args(batch=batch, dtype=0, cache_dtype=2 if bits == 8 else 0, num_q_heads=4, k_stride=128, v_stride=128, q_stride=256, q_out_stride=256)
+        a.q = b.q = box.put(c["q"])[1]
+        out, a.out = box.put(c["q_out"])
+        q_out, b.q_out = box.put(c["q_out"])
+        b.k, b.v = (box.put(torch.randn(N, H, D).bfloat16())[1] for _ in range(2))
+        if bits == 8:
+            scales, a.k_scale = box.put(c["scales"])
+            a.v_scale, a.scale_stride = a.k_scale + 4 * c["scales"][0].numel(), c["scales"].shape[2]
+            b.k_scale, b.v_scale, b.scale_stride = a.k_scale, a.v_scale, a.scale_stride
+        need = ctypes.c_size_t()
+        assert lib.kvio_attend_workspace(h, ctypes.byref(a), ctypes.byref(need)) == 0
+        a.workspace, a.workspace_bytes = box.put(torch.zeros(max(need.value, 16), dtype=torch.uint8))[1], need.value
+        assert lib.kvio_attend(h, 0, ctypes.byref(a), None) == 0, kv.kvio_last_error()
+        assert lib.kvio_append(h, 0, ctypes.byref(b), None) == 0, kv.kvio_last_error()
+        cut = [min(max(s, 0), N) for s in starts]
+        named = torch.zeros(N, dtype=torch.bool)
+        for i in range(3):
+            named[cut[i]:cut[i + 1]] = True
+        assert bool((out[~named] == -2.5).all()) and bool((q_out[~named] == -2.5).all())
+        pages = torch.zeros(c["pool"].shape[1] // P, dtype=torch.bool)
+        pages[c["table"][c["table"] >= 0].long()] = True
+        same = pool.view(torch.uint8).view(2, -1, P * H * D * pool.element_size()) == c["pool"].view(torch.uint8).view(2, -1, P * H * D * pool.element_size())
+        assert bool(same[:, ~pages].all())
+        kv.kvio_pool_destroy(h)
+        box.free()
