@@ -463,6 +463,8 @@ AttendPlan plan_steps(bool e4m3, int32_t heads, int32_t q_heads, int32_t dim, co
     const int64_t head_groups = heads / p.heads_per_group, splits = kWaves / p.heads_per_group;
     // As many workgroups as the GPU holds at once: 256 compute units, a wave on each SIMD for each of them.
     const int64_t most = std::max<int64_t>(256 * occupancy(e4m3, dim, p.columns) / head_groups, 1);
+    // With 2 or 8 tiles at least: 4 contexts of 2000 tokens of 32 heads 19.1 and 24.2 us (21.2 with 4), 8 drafts of 8 contexts of
+    // 3000 46.2 and 39.0 (43.4), 256 contexts of 200 44.7 and 50.9 (44.9).
     p.min_tiles = 4;
     const int64_t tiles = int64_t(b.num_seqs) * ((max_ctx + 2 * kTile - 1) / kTile);      // at most
     const int64_t workers = std::min(most * splits, (tiles + p.min_tiles - 1) / p.min_tiles);
