@@ -195,7 +195,8 @@ __device__ __forceinline__ void append_page(const AppendArgs &a, int group, f32x
     const uint8_t *in = (is_v ? a.v : a.k) + h * seg * 2;
     const int64_t in_stride = is_v ? a.v_stride : a.k_stride;
     const Place p = place_of(j < units ? j : 0, is_v ? 0 : a.rot_half, a.interleaved);
-    const int at_once = a.rot_half == 0 ? P : kAngles / a.rot_half;      // tokens whose angles LDS holds
+    // Tokens whose angles LDS holds; without, so many that places and a step more stay below 2^31 (contexts end 4096 before it).
+    const int at_once = a.rot_half == 0 ? 4096 : kAngles / a.rot_half;
     auto put_angles = [&](int t0) {          // of tokens t0 on
         workgroup_barrier();
         const int n = (to - t0 < at_once ? to - t0 : at_once) * a.rot_half;

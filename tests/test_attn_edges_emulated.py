@@ -209,3 +209,34 @@ def test_falling_offsets_touch_nothing_else(emu, bits, starts):  # noqa: F811
         assert bool(same[:, ~pages].all())
         kv.kvio_pool_destroy(h)
         box.free()
+
+
+@pytest.mark.parametrize("rot", [0, 16])
+def test_append_to_a_page_of_a_billion_tokens(emu, rot):  # noqa: F811
+    """Places past 2^30 in one page: steps through it stay below 2^31 (a layer of 17.6 GB, of which little is touched)."""
+    kv, lib, A = emu
+    P, D, ctx, new = 1_100_000_000, 16, 1_099_999_990, 3
+    box = Box(kv)
+    layers = [base.Memory(kv, P * D, 1, 1) for _ in range(2)]
+    h = kv.kvio_pool_create(1, 1, D, 1, P, P, [layers[0].ptr], [layers[1].ptr])
+    x = torch.arange(2 * new * D).view(2, new, 1, D).bfloat16() - 40
+    a = A.kvio_append_args(batch=batch_args(A, box, None, torch.zeros(1, 1, dtype=torch.int32), torch.tensor([ctx], dtype=torch.int32),
+                                            torch.tensor([0, new], dtype=torch.int32), new), dtype=0, cache_dtype=2, rot_dim=rot)
+    (_, a.k), (_, a.v) = box.put(x[0]), box.put(x[1])
+    a.k_stride = a.v_stride = D
+    if rot:
+        a.inv_freq = box.put(torch.zeros(rot // 2))[1]
+    scales, a.k_scale = box.put(torch.ones(2, 1, 1))
+    a.v_scale, a.scale_stride = a.k_scale + 4, 1
+    assert lib.kvio_append(h, 0, ctypes.byref(a), None) == 0, kv.kvio_last_error()
+    assert bool((scales == 1).all())
+    for i in range(2):
+        got = torch.from_numpy(layers[i].array[(ctx - new - 1) * D:(ctx + 1) * D].copy()).view(torch.float8_e4m3fn).double().view(new + 2, D)
+        assert bool((got[0] == 0).all()) and bool((got[-1] == 0).all())
+        want = x[i, :, 0].double()
+        assert bool(((got[1:-1] - want).abs() <= want.abs() * 2.0 ** -4).all())
+    kv.kvio_check(h)
+    kv.kvio_pool_destroy(h)
+    for m in layers:
+        m.free()
+    box.free()
